@@ -25,9 +25,6 @@ struct OrthoScales {
     float linear, unit;        // A sa -> b A sa sc, and a sa sc: what is added to the sum of A sa by c A sc
     float factor;              // that sum -> F sf
     float direct_linear, direct_unit;   // Y Y^T -> b A sf, and a sf: where c is 0
-    // the same for sums that start from (b A + a I) / c (where c is 0: from b A + a I, and nothing is added)
-    float small_linear, small_unit, small_factor;
-    int small_square;
     float apply;               // F Y -> the next Y, scaled
     float out;                 // the next Y, scaled -> its value
 };
@@ -71,8 +68,11 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(const void *__restrict_
     if (threadIdx.x == 0) sums[blockIdx.x] = wave_sums[0] + wave_sums[1] + wave_sums[2] + wave_sums[3];
 }
 
-// 1 / (norm + eps); 0 for a matrix of zeros, which stays one whatever eps is
-__device__ __forceinline__ double ortho_inverse(double squares, double eps) { return squares == 0.0 ? 0.0 : 1.0 / (sqrt(squares) + eps); }
+// 1 / (norm + eps); 0 for a matrix of zeros, which stays one whatever eps is; NaN for one with an infinity or a NaN
+__device__ __forceinline__ double ortho_inverse(double squares, double eps)
+{
+    return squares == 0.0 ? 0.0 : squares < HUGE_VAL ? 1.0 / (sqrt(squares) + eps) : __builtin_nan("");
+}
 
 // 1 / (norm + eps) of every matrix, a wavefront each.
 __global__ __launch_bounds__(64) void ortho_inverse_kernel(const double *__restrict__ sums, int parts, double eps, double *__restrict__ inverse)

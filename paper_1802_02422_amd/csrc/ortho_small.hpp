@@ -3,10 +3,12 @@
 //
 // A wavefront owns 32 rows of Y (MB wavefronts, Y of up to 32 MB x 32 NB).  Every product is formed with the shared operand's rows as the
 // first operand, from LDS, and the wavefront's own rows as the second, from registers, so that a lane's accumulators run along its own row:
-// exchanged between the halves of the wavefront they are fragments again (own_fragments).  4096 x 96 x 96, ten steps: 820 us (the same by
-// a launch for every product: 7.6 ms), products 300, terms 210 and LDS 280 of it in turn; 12 wavefronts a compute unit, with 6 of them and no spills 930.  LDS holds one matrix at a time, Y or A as
-// terms, which for 96 x 96 is 37 KB.  Y stands in LDS once for both of its uses: along
-// its rows for A = Y Y^T, and by transposing reads for F Y.
+// exchanged between the halves of the wavefront they are fragments again (own_fragments).  LDS holds one matrix at a time, Y or A as
+// terms, which for 96 x 96 is 37 KB.  Y stands in LDS once for both of its uses: along its rows for A = Y Y^T, and by transposing reads for F Y.
+//
+// Scales are powers of two that bring a matrix's largest element, as it is, to 2^13 .. 2^15: of A the largest on its diagonal, of F that of a wavefront's own
+// rows (nobody else has them), of Y that of all of it.  So nothing has to be known of the coefficients: what bounds of the singular values would allow drifts away from what
+// they are when a matrix shrinks for many steps, and two fp16 terms hold 22 bits only of what is within 2^18 of their scale.
 #pragma once
 #include "direct.hpp"
 #include "ortho.hpp"
@@ -14,7 +16,9 @@
 namespace ivf {
 
 constexpr int ORTHO_SMALL_SIDE = 128;
-constexpr int ORTHO_SMALL_STEPS = 64;
+constexpr int ORTHO_SMALL_STEPS = 256;                        // whose coefficients are arguments of the launch
+constexpr int ORTHO_TOP = 14;                                 // exponent of a scaled matrix's largest element
+constexpr int NOTHING = -(1 << 20);                           // in the place of an exponent: all zeros
 
 struct OrthoSmallArgs {
     const void *x;
@@ -22,9 +26,31 @@ struct OrthoSmallArgs {
     int rows, cols, steps, turned;                            // turned: Y is X transposed
     Type type;
     double eps;
-    float first;                                              // the first Y's scale
-    OrthoScales scales[ORTHO_SMALL_STEPS];
+    const float *more;                                        // more steps: where their coefficients are
+    float coefs[3 * ORTHO_SMALL_STEPS];
 };
+
+// Coefficients into memory: the arguments of a launch hold no more than these.
+struct OrthoCoefs {
+    float *to;
+    int count;
+    float coefs[3 * ORTHO_SMALL_STEPS];
+};
+
+__global__ __launch_bounds__(256) void ortho_coefs_kernel(OrthoCoefs c)
+{
+    for (int i = threadIdx.x; i < c.count; i += 256) c.to[i] = c.coefs[i];
+}
+
+// What takes a value of those magnitude bits to 2^ORTHO_TOP: the power of two's exponent.
+__device__ __forceinline__ int ortho_shift(uint32_t top)
+{
+    const int e = ORTHO_TOP + 127 - (int)(top >> 23);
+    return top == 0 ? 0 : e > 126 ? 126 : e;
+}
+
+__device__ __forceinline__ float ortho_power(int e) { return ldexpf(1.f, e); }
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
 // A fragment: 16 elements along a row, 8 of them in a lane.
 struct Terms {
@@ -105,12 +131,14 @@ struct OrthoSmall {
     }
 
     template <Type T>
-    static __device__ __forceinline__ double squares(const void *x, int64_t at, int size)
+    static __device__ __forceinline__ double squares(const void *x, int64_t at, int size, uint32_t &top)
     {
         double s = 0.0;
         for (int i = threadIdx.x; i < size; i += NT) {
-            const double v = element<T>(x, at + i);
+            const float f = element<T>(x, at + i);
+            const double v = f;
             s += v * v;
+            top = magnitude(f) > top ? magnitude(f) : top;
         }
         return s;
     }
@@ -133,43 +161,51 @@ struct OrthoSmall {
         }
     }
 
-    // Y from LDS to X's shape, in runs of four along X's rows
-    static __device__ __forceinline__ void give(const OrthoSmallArgs &g, int64_t at, int m, int n, float by, const uint16_t *lds)
+    // Where an element of the result stands in LDS: in 32 bits, which is as much as its two terms, runs of four exchanged by the row's number.
+    static __device__ __forceinline__ int place(int row, int col) { return row * N + (((col / 4) ^ (row & 7)) * 4) + col % 4; }
+
+    // the result from LDS to X's shape, in runs of four along X's rows
+    static __device__ __forceinline__ void give(const OrthoSmallArgs &g, int64_t at, int m, int n, const float *lds)
     {
         const int rows = g.turned ? n : m, cols = g.turned ? m : n, runs = (cols + 3) / 4;
         for (int id = threadIdx.x; id < rows * runs; id += NT) {
             const int r = id / runs, c = id % runs * 4;
             floatx4 v;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int row = g.turned ? c + j : r, col = g.turned ? r : c + j;   // (up to three past the end, inside the padding)
-                v[j] = 0.f;
-#pragma unroll
-                for (int t = TERMS - 1; t >= 0; --t)
-                    v[j] += (float)__builtin_bit_cast(_Float16, lds[t * (M * N) + line_at<N>(row, col / 8) + (col & 7)]);
-                v[j] *= by;
-            }
+            for (int j = 0; j < 4; ++j) v[j] = lds[g.turned ? place(c + j, r) : place(r, c + j)];   // (up to three past the end, inside the padding)
             put4(g.out, at + (int64_t)r * cols + c, v, cols - c, g.type);
         }
     }
 
-    __device__ __forceinline__ void run(const OrthoSmallArgs &g, uint16_t *lds, double *sums)
+    __device__ __forceinline__ void run(const OrthoSmallArgs &g, uint16_t *lds, double *sums, int *tops)
     {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / WAVE));
         const int64_t matrix = blockIdx.x, size = (int64_t)g.rows * g.cols;
         const int m = g.turned ? g.cols : g.rows, n = g.turned ? g.rows : g.cols;
+        // the largest of what the wavefronts have put into tops
+        auto largest = [&]() {
+            int v = tops[0];
+#pragma unroll
+            for (int w = 1; w < MB; ++w) v = tops[w] > v ? tops[w] : v;
+            return __builtin_amdgcn_readfirstlane(v);
+        };
         double s = 0.0;
-        if (g.type == Type::F32) s = squares<Type::F32>(g.x, matrix * size, (int)size);
-        else if (g.type == Type::F16) s = squares<Type::F16>(g.x, matrix * size, (int)size);
-        else s = squares<Type::BF16>(g.x, matrix * size, (int)size);
+        uint32_t top = 0;
+        if (g.type == Type::F32) s = squares<Type::F32>(g.x, matrix * size, (int)size, top);
+        else if (g.type == Type::F16) s = squares<Type::F16>(g.x, matrix * size, (int)size, top);
+        else s = squares<Type::BF16>(g.x, matrix * size, (int)size, top);
 #pragma unroll
         for (int o = WAVE / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, WAVE);
-        if (lane == 0) sums[wave] = s;
+        top = wave_extreme<true>(top);
+        if (lane == 0) sums[wave] = s, tops[wave] = (int)top;
         __syncthreads();
         s = 0.0;
 #pragma unroll
         for (int w = 0; w < MB; ++w) s += sums[w];
-        const double by = g.first * ortho_inverse(s, g.eps);
+        const double inverse = ortho_inverse(s, g.eps);
+        // Y's elements are y 2^-ey of the scaled ones
+        int ey = (int)(ORTHO_TOP + 1023 - (__double_as_longlong((double)__uint_as_float((uint32_t)largest()) * inverse) >> 52 & 2047));
+        const double by = ldexp(inverse, ey);
         if (g.type == Type::F32) bring<Type::F32>(g, matrix * size, m, n, by, lds);
         else if (g.type == Type::F16) bring<Type::F16>(g, matrix * size, m, n, by, lds);
         else bring<Type::BF16>(g, matrix * size, m, n, by, lds);
@@ -180,8 +216,12 @@ struct OrthoSmall {
             for (int p = 0; p < 2 * NB; ++p)
                 y[t][p] = *reinterpret_cast<const wordx4 *>(lds + t * (M * N) + line_at<N>(32 * wave + (lane & 31), 2 * p + lane / 32));
 
-        for (int step = 0; step < g.steps; ++step) {
-            const OrthoScales &sc = g.scales[step];
+        floatx16 next[NB];                                    // the next Y: 2^fe of these
+        int fe;
+        uint32_t high;
+        for (int step = 0;; ++step) {
+            const float ca = g.more ? g.more[3 * step] : g.coefs[3 * step], cb = g.more ? g.more[3 * step + 1] : g.coefs[3 * step + 1],
+                        cc = g.more ? g.more[3 * step + 2] : g.coefs[3 * step + 2];
             floatx16 a[MB];
 #pragma unroll
             for (int i = 0; i < MB; ++i) a[i] = zero();
@@ -194,28 +234,57 @@ struct OrthoSmall {
 #pragma unroll
                 for (int i = 0; i < MB; ++i) a[i] = products(row_fragment<N>(lds, 32 * i, p), v, a[i]);
             }
+            high = 0;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (i == wave && 8 * (e / 4) + 4 * (lane / 32) + e % 4 == (lane & 31)) high = magnitude(a[i][e]);
+            high = wave_extreme<true>(high);
+            if (lane == 0) tops[wave] = (int)high;
             __syncthreads();                                  // Y has been read
+            high = (uint32_t)largest();
+            const int to_a = ortho_shift(high), ea = 2 * ey + to_a;
+            // F = factor 2^fe (sums): those start from what is left of b A + a I.  Over c, so that c A A is their products of A's terms, unless it is below
+            // what 32 bits keep of the rest (which the sums could not hold over c either).
+            const double T = fmin(ldexp((double)__uint_as_float(high), -2 * ey), 1e300), rest = fabs((double)ca) + fabs((double)cb) * T;
+            const bool square = fabs((double)cc) * T * T >= 0x1p-60 * rest && cc != 0.f;
+            const int unit = (int)(1022 - (__double_as_longlong(rest) >> 52 & 2047));
+            const double over = square ? 1.0 / (double)cc : 1.0;
+            const float start_unit = (float)ldexp(ca * over, square ? 2 * ea : unit), start_linear = (float)ldexp(cb * over, square ? 2 * to_a + 2 * ey : unit - 2 * ey);
+            const float factor = square ? cc : 1.f;
+            fe = square ? -2 * ea : -unit;
+            const float scale_a = ortho_power(to_a);
 #pragma unroll
             for (int i = 0; i < MB; ++i) {
                 Terms t2[2];
-                own_fragments(a[i], sc.gram, t2);
+                own_fragments(a[i], scale_a, t2);
 #pragma unroll
                 for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
                     for (int t = 0; t < TERMS; ++t) put<M>(lds, t, 2 * i + s2, t2[s2].t[t]);
-                // what c A A comes to: (b A + a I), over c where there is A A
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    a[i][e] = sc.small_linear * a[i][e] + (i == wave && 8 * (e / 4) + 4 * (lane / 32) + e % 4 == (lane & 31) ? sc.small_unit : 0.f);
+                    a[i][e] = start_linear * a[i][e] + (i == wave && 8 * (e / 4) + 4 * (lane / 32) + e % 4 == (lane & 31) ? start_unit : 0.f);
             }
             __syncthreads();
-            if (sc.small_square)
+            if (square)
 #pragma unroll
                 for (int p = 0; p < 2 * MB; ++p) {
                     const Terms v = row_fragment<M>(lds, 32 * wave, p);
 #pragma unroll
                     for (int i = 0; i < MB; ++i) a[i] = products(row_fragment<M>(lds, 32 * i, p), v.t, a[i]);
                 }
+            high = 0;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) high = magnitude(a[i][e]) > high ? magnitude(a[i][e]) : high;
+            // (times c here, not later: near its fixed point the factor is close to the identity, which one term holds as it is)
+            high = wave_extreme<true>(high);
+            const int to_f = high ? ORTHO_TOP + 253 - (int)(high >> 23) - (int)(magnitude(factor) >> 23) : 0;
+            const float scale_f = ldexpf(factor, to_f);
+            fe -= to_f;
             __syncthreads();                                  // A has been read
             put_y(lds);
             __builtin_amdgcn_sched_barrier(0);                // (Y's registers are free for F)
@@ -223,7 +292,7 @@ struct OrthoSmall {
 #pragma unroll
             for (int i = 0; i < MB; ++i) {
                 Terms t2[2];
-                own_fragments(a[i], sc.small_factor, t2);
+                own_fragments(a[i], scale_f, t2);
 #pragma unroll
                 for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
@@ -231,10 +300,9 @@ struct OrthoSmall {
             }
             __syncthreads();
             // own rows of F Y: column block by column block, Y's columns as the first operand
-            wordx4 next[TERMS][2 * NB];
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
-                floatx16 acc = zero();
+                next[j] = zero();
 #pragma unroll
                 for (int p = 0; p < 2 * MB; ++p) {
                     Terms u;
@@ -252,35 +320,59 @@ struct OrthoSmall {
                         }
                         v[t] = f[t][p];
                     }
-                    acc = products(u, v, acc);
+                    next[j] = products(u, v, next[j]);
                 }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            high = 0;
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) high = magnitude(next[j][e]) > high ? magnitude(next[j][e]) : high;
+            high = wave_extreme<true>(high);
+            fe -= ey;
+            if (lane == 0) tops[wave] = high == 0 ? NOTHING : (int)(high >> 23) - 127 + fe;
+            __syncthreads();                                  // the old Y has been read
+            if (step + 1 == g.steps) break;
+            const int e = largest();
+            ey = e == NOTHING ? 0 : ORTHO_TOP - e;
+            const float scale_y = high ? ortho_power(fe + ey) : 0.f;
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
                 Terms t2[2];
-                own_fragments(acc, sc.apply, t2);
+                own_fragments(next[j], scale_y, t2);
 #pragma unroll
                 for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
-                    for (int t = 0; t < TERMS; ++t) next[t][2 * j + s2] = t2[s2].t[t];
-                __builtin_amdgcn_sched_barrier(0);
+                    for (int t = 0; t < TERMS; ++t) y[t][2 * j + s2] = t2[s2].t[t];
             }
-#pragma unroll
-            for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-                for (int p = 0; p < 2 * NB; ++p) y[t][p] = next[t][p];
-            __syncthreads();                                  // the old Y has been read
             put_y(lds);
             __syncthreads();
         }
-        give(g, matrix * size, m, n, g.scales[g.steps - 1].out, lds);
+        const float half = high ? ortho_power(fe / 2) : 0.f, other = high ? ortho_power(fe - fe / 2) : 0.f;   // (no infinity times zero)
+        float *result = reinterpret_cast<float *>(lds);
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                floatx4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = next[j][4 * q + e] * half * other;
+                *reinterpret_cast<floatx4 *>(result + place(32 * wave + (lane & 31), 32 * j + 8 * q + 4 * (lane / 32))) = v;
+            }
+        __syncthreads();
+        give(g, matrix * size, m, n, result);
     }
 };
 
 template <int MB, int NB>
-__global__ __launch_bounds__(WAVE *MB) __attribute__((amdgpu_waves_per_eu(MB + NB <= 6 ? 3 : 2))) void ortho_small_kernel(OrthoSmallArgs g)
+__global__ __launch_bounds__(WAVE *MB) __attribute__((amdgpu_waves_per_eu(NB <= 3 ? 3 : 2))) void ortho_small_kernel(OrthoSmallArgs g)
 {
     __shared__ __attribute__((aligned(16))) uint16_t lds[OrthoSmall<MB, NB>::LDS_HALVES];
     __shared__ double sums[MB];
+    __shared__ int tops[MB];
     OrthoSmall<MB, NB> s;
-    s.run(g, lds, sums);
+    s.run(g, lds, sums, tops);
 }
 
 }  // namespace ivf

@@ -180,6 +180,8 @@ extern "C" int ivf_grouped_gradient(const void *dy, int64_t lddy, const void *x,
 
 namespace {
 
+constexpr int ORTHO_MOST_STEPS = 1000;
+
 struct OrthoPlan {
     int m, n, ldm, ldn, parts;
     int64_t y, yt, f, sums, total;                            // bytes
@@ -201,7 +203,7 @@ int ortho_plan(int64_t batch, int rows, int cols, int type, OrthoPlan &p)
     p.yt = whole(batch * ORTHO_TERMS * p.n * p.ldm * 2);
     p.f = whole(batch * ORTHO_TERMS * p.m * p.ldm * 2);
     p.sums = whole(batch * (p.parts + 1) * 8);                // and an inverse norm each
-    p.total = p.y + 2 * p.yt + 2 * p.f + p.sums;
+    p.total = std::max<int64_t>(p.y + 2 * p.yt + 2 * p.f + p.sums, 3 * ORTHO_MOST_STEPS * sizeof(float));
     return IVF_OK;
 }
 
@@ -240,11 +242,6 @@ OrthoScales ortho_scales(const float *coefs, double &S)
     s.factor = (float)(sf / (sa * sc));
     s.direct_linear = (float)(b * sf / (sy * sy));
     s.direct_unit = (float)(a * sf);
-    s.small_square = c != 0.0;
-    const double over = c != 0.0 ? c : 1.0;
-    s.small_linear = (float)(b / over * sa * sa / (sy * sy));
-    s.small_unit = (float)(a / over * sa * sa);
-    s.small_factor = (float)(over * sf / (sa * sa));
     s.apply = (float)(sn / (sf * sy));
     s.out = (float)(1.0 / sn);
     return s;
@@ -379,7 +376,7 @@ extern "C" int ivf_orthogonalise(const void *x, int64_t batch, int rows, int col
     OrthoPlan p;
     if (int rc = ortho_plan(batch, rows, cols, type, p)) return rc;
     if (!coefs || (batch > 0 && (!x || !out))) return fail(IVF_EINVAL, "NULL argument");
-    if (steps < 1 || steps > 1000) return fail(IVF_EINVAL, "steps=%d out of range", steps);
+    if (steps < 1 || steps > ORTHO_MOST_STEPS) return fail(IVF_EINVAL, "steps=%d out of range", steps);
     if (!(eps >= 0.f) || eps > 1e30f) return fail(IVF_EINVAL, "eps must be finite and not negative");
     for (int i = 0; i < 3 * steps; ++i)
         if (!std::isfinite(coefs[i])) return fail(IVF_EINVAL, "a coefficient is not finite");
@@ -389,21 +386,22 @@ extern "C" int ivf_orthogonalise(const void *x, int64_t batch, int rows, int col
     if (!aligned(workspace, 16)) return fail(IVF_EINVAL, "workspace must be 16-byte aligned");
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
-    // (a factor that is divided by its last coefficient has to stay within fp32's range)
-    const bool bounded = ortho_bounded(steps, coefs);
-    bool small = bounded && rows <= ORTHO_SMALL_SIDE && cols <= ORTHO_SMALL_SIDE && steps <= ORTHO_SMALL_STEPS;
-    for (int i = 0; i < steps && small; ++i) {
-        const double c = std::fabs(coefs[3 * i + 2]);
-        small = c == 0.0 || std::fabs(coefs[3 * i]) + std::fabs(coefs[3 * i + 1]) <= c * 0x1p40;
-    }
-    if (small) {
-        OrthoSmallArgs a{x, out, rows, cols, steps, rows > cols, type_of(type), eps, (float)ortho_scale(1.0), {}};
-        double S = 1.0;
-        for (int i = 0; i < steps; ++i) {
-            a.scales[i] = ortho_scales(coefs + 3 * i, S);
+    if (rows <= ORTHO_SMALL_SIDE && cols <= ORTHO_SMALL_SIDE) {
+        OrthoSmallArgs a{x, out, rows, cols, steps, rows > cols, type_of(type), eps, nullptr, {}};
+        if (steps <= ORTHO_SMALL_STEPS) {
+            std::copy(coefs, coefs + 3 * steps, a.coefs);
+        } else {
+            a.more = static_cast<const float *>(workspace);
+            for (int i = 0; i < steps; i += ORTHO_SMALL_STEPS) {
+                OrthoCoefs c{static_cast<float *>(workspace) + 3 * i, 3 * std::min(ORTHO_SMALL_STEPS, steps - i), {}};
+                std::copy(coefs + 3 * i, coefs + 3 * i + c.count, c.coefs);
+                ortho_coefs_kernel<<<dim3(1), dim3(256), 0, st>>>(c);
+                LAUNCHCHK("ortho_coefs_kernel");
+            }
         }
         return ortho_small(a, batch, st);
     }
+    const bool bounded = ortho_bounded(steps, coefs);
     return by_type(type, [&](auto t) -> int {
         constexpr Type T = decltype(t)::value;
         if (!bounded) return ortho_general<T>(x, batch, rows, cols, steps, coefs, eps, out, p, ws, st);

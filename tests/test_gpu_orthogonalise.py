@@ -1,0 +1,88 @@
+"""Orthogonalising steps where scales and sums decide: runs of steps that shrink a matrix, matrices far below eps, shapes of every tile
+(needs an MI355X).
+
+Tolerances.  A matrix in two fp16 terms is within 2^-22 of itself, and a product leaves as much out; its fp32 sums round by 2^-23 of the sum so far,
+three times for 16 products, with random signs: for up to 512 products like sqrt(3 x 33) < 10 of them at once.  A product is thus within 8 x 2^-22 of the size of
+what it is made of (for signs at random ||A|| ||Y||_F, A's largest singular value), and a step with its three products within 24 x 2^-22 of (|a| + |b| s^2 + |c| s^4) f, s
+the largest singular value and f = ||X||_F.  Sums of more products count as their root.  An error that is there already is multiplied by the largest
+derivative |a + 3 b t^2 + 5 c t^4| or quotient |a + b t^2 + c t^4| over singular values t up to s.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import paper_1802_02422_amd as ivf
+
+F32 = torch.float32
+POLAR, UPDATE = [(1.875, -1.25, 0.375)] * 12, [(3.4445, -4.775, 2.0315)] * 5
+STEP = 24 * 2.0 ** -22
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def reference(x, coefs, eps):
+    """(the result in 64 bits, the bound of the head for its error's norm) of every matrix."""
+    y = x.double()
+    y = y / (y.flatten(-2).norm(dim=-1)[..., None, None] + eps)
+    tol = torch.zeros(y.shape[:-2], dtype=torch.float64, device=y.device)
+    unit = STEP * max(1.0, math.sqrt(max(y.shape[-2:]) / 512))
+    grid = torch.linspace(0, 1, 2001, dtype=torch.float64, device=y.device)
+    for a, b, c in coefs:
+        turned = y.shape[-2] > y.shape[-1]
+        A = y.mT.contiguous() @ y if turned else y @ y.mT.contiguous()
+        f, s = y.flatten(-2).norm(dim=-1), torch.linalg.eigvalsh(A)[..., -1].clamp(min=0).sqrt()
+        t = (grid * s[..., None]) ** 2
+        grow = torch.maximum((a + 3 * b * t + 5 * c * t * t).abs(), (a + b * t + c * t * t).abs()).amax(-1)
+        tol = tol * grow + unit * (abs(a) + abs(b) * s ** 2 + abs(c) * s ** 4) * f
+        F = b * A + c * (A @ A)
+        y = a * y + (y @ F if turned else F @ y)
+    return y, tol
+
+
+def check(x, coefs, eps=1e-7, dtype=F32):
+    x = x.to(dtype)
+    ref, tol = reference(x, coefs, eps)
+    got = ivf.ivf_orthogonalise(x.cuda(), coefs, eps=eps).to(x.device)
+    size = ref.flatten(-2).norm(dim=-1)
+    last = {F32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}[dtype]
+    err = (got.double() - ref).flatten(-2).norm(dim=-1)
+    print("relative error", (err / size).max().item(), "bound", (tol / size + last).max().item(), flush=True)
+    assert got.dtype == dtype and got.isfinite().all()
+    assert (err <= tol + last * size).all()
+
+
+LONG = {"no_linear_growth": [(0.5, 0.0, 1e-3)] * 24, "tiny_last": [(0.5, 0.0, 1e-11)] * 18, "shrink_30": [(0.5, 0.5, 0.0)] * 30,
+        "shrink_40": [(0.6, 0.4, 0.0)] * 40, "halves": [(0.5, 0.0, 0.0)] * 60, "down_then_up": [(0.5, 0.5, 0.0)] * 20 + [(2.0, 0.0, 0.0)] * 20,
+        "only_last": [(0.0, 0.0, 1.0)] * 2, "sign": [(-0.7, 0.2, 0.1)] * 50, "more_than_an_argument": [(0.9, 0.05, 0.01)] * 300,
+        "grow": [(1.5, 0.3, 0.2)] * 3}
+SMALL = [(2, 40, 24), (3, 96, 96), (1, 1, 1), (2, 128, 70)]
+
+
+@pytest.mark.parametrize("coefs", LONG, ids=list(LONG))
+@pytest.mark.parametrize("shape", SMALL)
+def test_runs_of_steps_on_small_matrices(coefs, shape):
+    """The values leave their bounds behind: what is computed keeps its accuracy relative to what is left."""
+    print("case:", coefs, shape, flush=True)
+    check(torch.randn(*shape, generator=gen(len(coefs))), LONG[coefs], eps=0.0)
+
+
+@pytest.mark.parametrize("size,eps", [(1e-30, 1e-7), (1e-4, 1.0), (1e-12, 1e-7), (1e20, 1e3)])
+def test_small_matrices_far_below_eps(size, eps):
+    print("case: below eps", size, eps, flush=True)
+    check(torch.randn(4, 50, 33, generator=gen(3)) * size, POLAR[:5], eps=eps)
+    check(torch.randn(2, 20, 96, generator=gen(4)) * size, UPDATE, eps=eps)
+
+
+def test_small_matrices_infinite_or_not_a_number():
+    """Whatever the coefficients: all of the matrix, and no other."""
+    print("case: infinite", flush=True)
+    for coefs in (POLAR[:3], [(1.5, -0.5, 0.0)] * 2, [(2.0, 0.0, 0.0)], [(0.0, 0.0, 1.0)]):
+        x = torch.randn(4, 30, 40, generator=gen(5))
+        x[1, 3, 4], x[2, 29, 39] = float("inf"), float("nan")
+        got = ivf.ivf_orthogonalise(x.cuda(), coefs).cpu()
+        assert got[[1, 2]].isnan().all() and got[[0, 3]].isfinite().all()
