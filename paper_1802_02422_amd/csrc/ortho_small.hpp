@@ -93,14 +93,19 @@ struct OrthoSmall {
         return z;
     }
 
-    static __device__ __forceinline__ floatx16 products(const Terms &a, const wordx4 (&b)[TERMS], floatx16 acc)
+    // acc += a b; the products with a low term, a thousandth of the others, go into a sum of their own, so that acc is rounded once where it would be three times
+    static __device__ __forceinline__ void multiply(const Terms &a, const wordx4 (&b)[TERMS], floatx16 &acc, floatx16 &low)
+    {
+        low = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, a.t[0]), __builtin_bit_cast(halfx8, b[1]), low, 0, 0, 0);
+        low = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, a.t[1]), __builtin_bit_cast(halfx8, b[0]), low, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, a.t[0]), __builtin_bit_cast(halfx8, b[0]), acc, 0, 0, 0);
+    }
+
+    static __device__ __forceinline__ void add(floatx16 &acc, const floatx16 &low)
     {
 #pragma unroll
-        for (int order = TERMS - 1; order >= 0; --order)
-#pragma unroll
-            for (int t = 0; t <= order; ++t)
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, a.t[t]), __builtin_bit_cast(halfx8, b[order - t]), acc, 0, 0, 0);
-        return acc;
+        for (int e = 0; e < 16; ++e) acc[e] += low[e];
+        __builtin_amdgcn_sched_barrier(0);                    // (one block's fragments at a time)
     }
 
     // own rows into LDS
@@ -223,16 +228,19 @@ struct OrthoSmall {
             const float ca = g.more ? g.more[3 * step] : g.coefs[3 * step], cb = g.more ? g.more[3 * step + 1] : g.coefs[3 * step + 1],
                         cc = g.more ? g.more[3 * step + 2] : g.coefs[3 * step + 2];
             floatx16 a[MB];
-#pragma unroll
-            for (int i = 0; i < MB; ++i) a[i] = zero();
             // A = Y Y^T: columns of own rows
 #pragma unroll
-            for (int p = 0; p < 2 * NB; ++p) {
-                wordx4 v[TERMS];
+            for (int i = 0; i < MB; ++i) {
+                floatx16 low = zero();
+                a[i] = zero();
 #pragma unroll
-                for (int t = 0; t < TERMS; ++t) v[t] = y[t][p];
+                for (int p = 0; p < 2 * NB; ++p) {
+                    wordx4 v[TERMS];
 #pragma unroll
-                for (int i = 0; i < MB; ++i) a[i] = products(row_fragment<N>(lds, 32 * i, p), v, a[i]);
+                    for (int t = 0; t < TERMS; ++t) v[t] = y[t][p];
+                    multiply(row_fragment<N>(lds, 32 * i, p), v, a[i], low);
+                }
+                add(a[i], low);
             }
             high = 0;
 #pragma unroll
@@ -270,10 +278,11 @@ struct OrthoSmall {
             __syncthreads();
             if (square)
 #pragma unroll
-                for (int p = 0; p < 2 * MB; ++p) {
-                    const Terms v = row_fragment<M>(lds, 32 * wave, p);
+                for (int i = 0; i < MB; ++i) {
+                    floatx16 low = zero();
 #pragma unroll
-                    for (int i = 0; i < MB; ++i) a[i] = products(row_fragment<M>(lds, 32 * i, p), v.t, a[i]);
+                    for (int p = 0; p < 2 * MB; ++p) multiply(row_fragment<M>(lds, 32 * i, p), row_fragment<M>(lds, 32 * wave, p).t, a[i], low);
+                    add(a[i], low);
                 }
             high = 0;
 #pragma unroll
@@ -302,6 +311,7 @@ struct OrthoSmall {
             // own rows of F Y: column block by column block, Y's columns as the first operand
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
+                floatx16 low = zero();
                 next[j] = zero();
 #pragma unroll
                 for (int p = 0; p < 2 * MB; ++p) {
@@ -320,9 +330,9 @@ struct OrthoSmall {
                         }
                         v[t] = f[t][p];
                     }
-                    next[j] = products(u, v, next[j]);
+                    multiply(u, v, next[j], low);
                 }
-                __builtin_amdgcn_sched_barrier(0);
+                add(next[j], low);
             }
             high = 0;
 #pragma unroll

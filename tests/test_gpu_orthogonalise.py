@@ -86,3 +86,37 @@ def test_small_matrices_infinite_or_not_a_number():
         x[1, 3, 4], x[2, 29, 39] = float("inf"), float("nan")
         got = ivf.ivf_orthogonalise(x.cuda(), coefs).cpu()
         assert got[[1, 2]].isnan().all() and got[[0, 3]].isfinite().all()
+
+
+def plain(x, coefs):
+    y = x / (x.square().sum((1, 2), keepdim=True).sqrt() + 1e-7)
+    for a, b, c in coefs:
+        A = torch.bmm(y, y.transpose(1, 2).contiguous())
+        y = a * y + torch.bmm(b * A + c * torch.bmm(A, A), y)
+    return y
+
+
+@pytest.mark.parametrize("shape", [(64, 96, 96), (64, 64, 128)])
+@pytest.mark.parametrize("kind", ["diagonal", "noise", "rank3", "strong"])
+def test_small_matrices_as_accurate_as_32_bits(kind, shape):
+    """Against the same steps in fp32, whose sums of about a hundred products are off by some 2^-22 of their size; two terms (2^-22 at most, 2^-24.8 on average, of either
+    operand and as much left out) add a few per cent to that, so a fifth more is never reached unless sums are rounded more often."""
+    print("case: as 32 bits", kind, shape, flush=True)
+    b, r, k = shape
+    g = gen(17)
+    noise, low = torch.randn(b, r, k, generator=g), torch.randn(b, r, 3, generator=g) @ torch.randn(b, 3, k, generator=g)
+    d = torch.arange(min(r, k))
+    coefs = UPDATE
+    if kind == "diagonal":
+        x, coefs = 0.2 * noise / k ** 0.5, POLAR[:10]
+        x[:, d, d] += 0.3 + torch.rand(b, min(r, k), generator=g)
+    elif kind == "noise":
+        x = noise / k ** 0.5
+    elif kind == "rank3":
+        x = 1e-4 * noise + low / (r * k) ** 0.5
+    else:
+        x = noise / max(r, k) ** 0.5 + 4 * low / (r * k) ** 0.5
+    ref = reference(x, coefs, 1e-7)[0]
+    got, same = ivf.ivf_orthogonalise(x.cuda(), coefs).double().cpu() - ref, plain(x.cuda(), coefs).double().cpu() - ref
+    print("error", got.norm().item(), "in fp32", same.norm().item(), flush=True)
+    assert got.norm() <= 1.2 * same.norm()
