@@ -457,9 +457,9 @@ int ivf_grouped_gradient(const void *dy, int64_t lddy, const void *x, int64_t ld
  * towards 1 (the orthogonal factor: the rotation nearest to a
  * cross-covariance), with coefficients that grow small values faster to near 1 in
  * fewer steps (an optimiser's update of a weight).  The norm is summed in
- * fp64; between steps a matrix is held in 22 significant bits (two fp16 terms
- * under scales that follow from the coefficients; in fp32 where those may take
- * singular values past 16, or down by more than half).
+ * fp64; between steps a matrix is held in 22 significant bits, two fp16 terms
+ * under scales that follow the matrix (or, past 128 x 128, in fp32 where the
+ * coefficients of a step may take singular values past 16, or down by more than half).
  * A matrix of zeros stays zero; one with a NaN or an infinity becomes NaN.
  */
 int64_t ivf_orthogonalise_workspace(int64_t batch, int rows, int cols, int type);

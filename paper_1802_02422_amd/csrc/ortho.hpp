@@ -2,10 +2,11 @@
 // vectors as they are and move its singular values.  A is taken on the shorter side: Y is X, or X^T where X has more rows than columns.
 //
 // Terms.  Every matrix is kept as two fp16 terms, hi = fp16(x s) and lo = fp16(x s - hi), 22 significant bits, and products are formed as
-// lo hi + hi lo + hi hi in fp32: half the work of three bfloat16 terms.  That needs scales s that keep fp16's range, and there is a bound for every
-// one of them before the first step: |X|_2 <= |X|_F <= 1 to begin with, a step takes the singular values' bound S to the largest |a v + b v^3 + c v^5|
-// on [0, S], A is at most S^2 and the factor a I + b A + c A^2 the largest |a + b t + c t^2| on [0, S^2]; no element is larger than its
-// matrix's norm.  Scales are powers of two (ortho_scales).  Where the bounds say little (a step that may take singular values past 16, or small
+// lo hi + hi lo + hi hi in fp32: half the work of three bfloat16 terms.  That needs scales s that keep fp16's range, known before a matrix is written.  With S a bound of Y's
+// singular values A is at most S^2, the factor a I + b A + c A^2 the largest |a + b t + c t^2| on [0, S^2], and the next Y the largest |a v + b v^3 + c v^5| on [0, S]; no
+// element is larger than its matrix's norm.  S is the smaller of two: what the coefficients make of 1 from step to step, and ||Y||_F, which is summed while Y is written (||X||_F to
+// begin with).  Two terms hold 22 bits of what is within 2^18 of the scale, and the first alone would drift away from matrices that shrink.  Scales are powers of two.
+// Where a step's bounds say little (one that may take singular values past 16, or small
 // ones down faster than by half: ortho_bounded) matrices stay in fp32 and are multiplied as three bfloat16 terms.  One term would leave 2^-12, and after the growth of small singular values up to
 // 2.4e-3 of the result, more than a result in bfloat16 is rounded by; two leave 5e-7 (fp32 products of fp32 values: 3e-6).
 #pragma once
@@ -18,16 +19,45 @@ typedef _Float16 halfx4 __attribute__((ext_vector_type(4)));
 
 constexpr int ORTHO_TERMS = 2;
 
-// Multipliers of a step, the scales included (sy: of Y, sa: of A, sc: of c A, sf: of the factor F, sn: of the next Y)
+// Multipliers of a step, the scales included (sy: of Y, sa: of A, sf: of the factor F, sn: of the next Y)
 struct OrthoScales {
     float gram;                // Y Y^T -> A sa
-    float square;              // A sa -> c A sc
-    float linear, unit;        // A sa -> b A sa sc, and a sa sc: what is added to the sum of A sa by c A sc
-    float factor;              // that sum -> F sf
-    float direct_linear, direct_unit;   // Y Y^T -> b A sf, and a sf: where c is 0
-    float apply;               // F Y -> the next Y, scaled
-    float out;                 // the next Y, scaled -> its value
+    float square, linear, unit;         // the product of A sa by itself, A sa, the diagonal -> F sf
+    float direct_linear, direct_unit;   // Y Y^T, the diagonal -> F sf: where c is 0
+    float apply, last;         // F Y -> the next Y, scaled, or its value
+    double next;               // sn
 };
+
+// The power of two that takes values of up to `bound` to 2^15 at most.
+__host__ __device__ __forceinline__ double ortho_scale(double bound)
+{
+    if (!(bound > 0.0)) return 1.0;
+    const int e = bound < HUGE_VAL ? 14 - ilogb(bound) : 0;
+    return ldexp(1.0, e < -400 ? -400 : e > 400 ? 400 : e);
+}
+
+// The bounds of a step from S, that of the singular values before it: of the factor, and of the values after it.
+struct OrthoBounds {
+    double factor, next;
+};
+
+__host__ __device__ inline OrthoBounds ortho_bounds(double a, double b, double c, double S)
+{
+    const double T = S * S;
+    auto odd = [&](double t) { return fabs(sqrt(t) * (a + b * t + c * t * t)); };               // of a singular value whose square is t
+    auto even = [&](double t) { return fabs(a + b * t + c * t * t); };
+    OrthoBounds r{fmax(fabs(a), even(T)), odd(T)};
+    auto look = [&](double t) { if (t > 0.0 && t < T) r.next = fmax(r.next, odd(t)); };
+    if (c != 0.0) {
+        const double d = 9.0 * b * b - 20.0 * a * c;           // a + 3 b t + 5 c t^2 = 0
+        if (d >= 0.0) look((-3.0 * b + sqrt(d)) / (10.0 * c)), look((-3.0 * b - sqrt(d)) / (10.0 * c));
+        const double t = -b / (2.0 * c);
+        if (t > 0.0 && t < T) r.factor = fmax(r.factor, even(t));
+    } else if (b != 0.0) {
+        look(-a / (3.0 * b));
+    }
+    return r;
+}
 
 // Y is kept in both orientations because the products sum along rows of either.
 struct OrthoMatrix {
@@ -74,14 +104,47 @@ __device__ __forceinline__ double ortho_inverse(double squares, double eps)
     return squares == 0.0 ? 0.0 : squares < HUGE_VAL ? 1.0 / (sqrt(squares) + eps) : __builtin_nan("");
 }
 
-// 1 / (norm + eps) of every matrix, a wavefront each.
-__global__ __launch_bounds__(64) void ortho_inverse_kernel(const double *__restrict__ sums, int parts, double eps, double *__restrict__ inverse)
+// The sum of `parts` numbers, for every lane of a wavefront.
+__device__ __forceinline__ double ortho_sum(const double *sums, int parts)
 {
     double s = 0.0;
-    for (int i = threadIdx.x; i < parts; i += 64) s += sums[(int64_t)blockIdx.x * parts + i];
+    for (int i = threadIdx.x; i < parts; i += 64) s += sums[i];
 #pragma unroll
     for (int o = WAVE / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, WAVE);
-    if (threadIdx.x == 0) inverse[blockIdx.x] = ortho_inverse(s, eps);
+    return s;
+}
+
+// 1 / (norm + eps) of every matrix and its norm after that, a wavefront each.
+__global__ __launch_bounds__(64) void ortho_inverse_kernel(const double *__restrict__ sums, int parts, double eps, double *__restrict__ inverse, double *__restrict__ norms)
+{
+    const double s = ortho_sum(sums + (int64_t)blockIdx.x * parts, parts), by = ortho_inverse(s, eps);
+    if (threadIdx.x == 0) {
+        inverse[blockIdx.x] = by;
+        norms[blockIdx.x] = sqrt(s) * by;
+    }
+}
+
+// The multipliers of every matrix's next step, a wavefront each: of the first one (sums NULL) from norms, of others from the squares of the scaled Y that the last
+// step's workgroups have summed.  most: a bound of its singular values that follows from the coefficients.
+__global__ __launch_bounds__(64) void ortho_scales_kernel(const double *__restrict__ sums, int parts, const double *__restrict__ norms, double a, double b, double c,
+                                                          double most, OrthoScales *__restrict__ scales)
+{
+    const int64_t matrix = blockIdx.x;
+    OrthoScales &s = scales[matrix];
+    const double sy = sums ? s.next : ortho_scale(norms[matrix]);
+    const double S = fmin(most, sums ? sqrt(ortho_sum(sums + matrix * parts, parts)) / sy : norms[matrix]);
+    if (threadIdx.x != 0) return;
+    const OrthoBounds bound = ortho_bounds(a, b, c, S);
+    const double sa = ortho_scale(S * S), sf = ortho_scale(bound.factor), sn = ortho_scale(bound.next);
+    s.gram = (float)(sa / sy / sy);
+    s.square = (float)(c * sf / sa / sa);
+    s.linear = (float)(b * sf / sa);
+    s.unit = (float)(a * sf);
+    s.direct_linear = (float)(b * sf / sy / sy);
+    s.direct_unit = (float)(a * sf);
+    s.apply = (float)(sn / sf / sy);
+    s.last = (float)(1.0 / sf / sy);
+    s.next = sn;
 }
 
 // Terms of N values (N even), two a word.
@@ -103,13 +166,13 @@ __device__ __forceinline__ void ortho_cut(const float (&v)[N], uint32_t (&out)[O
 // x over its norm, scaled, as terms, in x's orientation (same) and transposed: 32 x 32 elements a workgroup.
 template <Type T>
 __global__ __launch_bounds__(256) void ortho_first_kernel(const void *__restrict__ x, int rows, int cols, const double *__restrict__ inverse,
-                                                          float scale, OrthoMatrix same, OrthoMatrix turned)
+                                                          const double *__restrict__ norms, OrthoMatrix same, OrthoMatrix turned)
 {
     __shared__ float tile[32][33];
     const int across = (cols + 31) / 32, down = (rows + 31) / 32;
     const int64_t matrix = blockIdx.x / (across * down);
     const int c0 = (int)(blockIdx.x % across) * 32, r0 = (int)(blockIdx.x / across % down) * 32;
-    const double by = scale * inverse[matrix];
+    const double by = ortho_scale(norms[matrix]) * inverse[matrix];
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
 #pragma unroll
     for (int i = 0; i < 32; i += 8) {
@@ -167,7 +230,7 @@ using OrthoTile = DirectTile<false, ORTHO_TERMS, B, W, false, ORTHO_TERMS, B, W,
 // Symmetric results, the tiles on and below the diagonal, each written to both sides.
 //   GRAM: to = Y Y^T, or a I + b Y Y^T (direct)      else: to = a I + b F + c F F, F symmetric
 template <int B, int W, bool GRAM>
-__global__ __launch_bounds__(WAVE *W *W) void ortho_symmetric_kernel(OrthoMatrix from, OrthoMatrix to, OrthoScales s, int direct)
+__global__ __launch_bounds__(WAVE *W *W) void ortho_symmetric_kernel(OrthoMatrix from, OrthoMatrix to, const OrthoScales *__restrict__ scales, int direct)
 {
     using P = OrthoTile<B, W>;
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
@@ -181,6 +244,7 @@ __global__ __launch_bounds__(WAVE *W *W) void ortho_symmetric_kernel(OrthoMatrix
     t.clear();
     t.product(ortho_source(from, matrix, i0), ortho_source(from, matrix, j0), from.ld, lds);
     const OrthoMatrix none{nullptr, 0, 0, 0};
+    const OrthoScales s = scales[matrix];
     t.each([&](int ri, int rj, floatx4 v) {
         const int row = j0 + rj, col = i0 + ri;
         if constexpr (GRAM) {
@@ -191,20 +255,18 @@ __global__ __launch_bounds__(WAVE *W *W) void ortho_symmetric_kernel(OrthoMatrix
             if (row < from.rows && col < from.ld) {
                 const uint16_t *f = from.at(matrix, row, col);
                 const halfx4 hi = *reinterpret_cast<const halfx4 *>(f), lo = *reinterpret_cast<const halfx4 *>(f + 32);
-                // (the sum is of A sa by A sa here: square takes it to A sa by c A sc)
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    v[q] = s.factor * (s.square * v[q] + s.linear * ((float)hi[q] + (float)lo[q]) + (row == col + q ? s.unit : 0.f));
+                for (int q = 0; q < 4; ++q) v[q] = s.square * v[q] + s.linear * ((float)hi[q] + (float)lo[q]) + (row == col + q ? s.unit : 0.f);
             }
         }
         put_terms(to, i0 == j0 ? none : to, matrix, row, col, v);
     });
 }
 
-// Y <- F Y from Y transposed: both orientations, or the result itself in x's (last).
+// Y <- F Y from Y transposed: both orientations and the sum of the squares of its scaled elements, or the result itself in x's (last).
 template <int B, int W>
-__global__ __launch_bounds__(WAVE *W *W) void ortho_apply_kernel(OrthoMatrix yt, OrthoMatrix f, OrthoMatrix to, OrthoMatrix to_t, float by, void *out,
-                                                                 Type type, int turned)
+__global__ __launch_bounds__(WAVE *W *W) void ortho_apply_kernel(OrthoMatrix yt, OrthoMatrix f, OrthoMatrix to, OrthoMatrix to_t, const OrthoScales *__restrict__ scales,
+                                                                 double *__restrict__ sums, void *out, Type type, int turned)
 {
     using P = OrthoTile<B, W>;
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
@@ -218,10 +280,15 @@ __global__ __launch_bounds__(WAVE *W *W) void ortho_apply_kernel(OrthoMatrix yt,
     t.clear();
     t.product(ortho_source(yt, matrix, j0), ortho_source(f, matrix, i0), f.ld, lds);
     const int m = f.rows, n = yt.rows;
+    const float by = out ? scales[matrix].last : scales[matrix].apply;
+    float squares = 0.f;
     t.each([&](int rj, int ri, floatx4 v) {
         const int row = i0 + ri, col = j0 + rj;                // of Y
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] *= by;
+        for (int q = 0; q < 4; ++q) {
+            v[q] *= by;
+            squares = row < m && col + q < n ? fmaf(v[q], v[q], squares) : squares;
+        }
         if (!out) {
             put_terms(to, to_t, matrix, row, col, v);
         } else if (row < m && col < n) {
@@ -232,6 +299,17 @@ __global__ __launch_bounds__(WAVE *W *W) void ortho_apply_kernel(OrthoMatrix yt,
                     if (col + q < n) put4(out, (matrix * n + col + q) * m + row, floatx4{v[q], 0.f, 0.f, 0.f}, 1, type);
         }
     });
+    if (out) return;
+    double *wave_sums = reinterpret_cast<double *>(lds);      // (nobody reads it any more)
+    const double s = wave_sum((double)squares);
+    if (threadIdx.x % WAVE == 0) wave_sums[threadIdx.x / WAVE] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double all = 0.0;
+#pragma unroll
+        for (int w = 0; w < W * W; ++w) all += wave_sums[w];
+        sums[matrix * (across * down) + i * across + j] = all;
+    }
 }
 
 // Coefficients without useful bounds: matrices in fp32, without padding.

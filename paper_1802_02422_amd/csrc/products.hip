@@ -183,7 +183,7 @@ namespace {
 constexpr int ORTHO_MOST_STEPS = 1000;
 
 struct OrthoPlan {
-    int m, n, ldm, ldn, parts;
+    int m, n, ldm, ldn, chunks, parts;
     int64_t y, yt, f, sums, total;                            // bytes
 };
 
@@ -197,76 +197,47 @@ int ortho_plan(int64_t batch, int rows, int cols, int type, OrthoPlan &p)
     p.ldm = (int)ceil_div(p.m, 32) * 32;
     p.ldn = (int)ceil_div(p.n, 32) * 32;
     const int64_t size = (int64_t)rows * cols;
-    p.parts = (int)ceil_div(size, NORM_CHUNK);
+    p.chunks = (int)ceil_div(size, NORM_CHUNK);
     auto whole = [](int64_t b) { return ceil_div(b, 256) * 256; };
     p.y = whole(batch * ORTHO_TERMS * p.m * p.ldn * 2);
     p.yt = whole(batch * ORTHO_TERMS * p.n * p.ldm * 2);
     p.f = whole(batch * ORTHO_TERMS * p.m * p.ldm * 2);
-    p.sums = whole(batch * (p.parts + 1) * 8);                // and an inverse norm each
+    // sums of squares by chunks of X or by tiles of Y, of 64 x 64 at least; of each matrix an inverse norm, a norm and the multipliers
+    p.parts = (int)std::max<int64_t>(p.chunks, ceil_div(p.m, 64) * ceil_div(p.n, 64));
+    p.sums = whole(batch * (p.parts * 8 + 16 + (int64_t)sizeof(OrthoScales)));
     p.total = std::max<int64_t>(p.y + 2 * p.yt + 2 * p.f + p.sums, 3 * ORTHO_MOST_STEPS * sizeof(float));
     return IVF_OK;
 }
 
-// The largest power of two that keeps values of up to `bound` within fp16's range, with room for rounding.
-double ortho_scale(double bound)
-{
-    if (!(bound > 0.0)) return 1.0;
-    const double e = std::floor(std::log2(30000.0 / bound));
-    return std::ldexp(1.0, (int)(e < -60.0 ? -60.0 : e > 60.0 ? 60.0 : e));
-}
-
-// The scales of a step from the bound S of the singular values before it (see ortho.hpp); S becomes the bound after it.
-OrthoScales ortho_scales(const float *coefs, double &S)
-{
-    const double a = coefs[0], b = coefs[1], c = coefs[2], T = S * S;
-    auto odd = [&](double t) { return std::fabs(std::sqrt(t) * (a + b * t + c * t * t)); };     // of a singular value whose square is t
-    auto even = [&](double t) { return std::fabs(a + b * t + c * t * t); };
-    double most = odd(T), factor = std::fmax(std::fabs(a), even(T));
-    auto look = [&](double t) { if (t > 0.0 && t < T) most = std::fmax(most, odd(t)); };
-    if (c != 0.0) {
-        const double d = 9.0 * b * b - 20.0 * a * c;           // a + 3 b t + 5 c t^2 = 0
-        if (d >= 0.0) look((-3.0 * b + std::sqrt(d)) / (10.0 * c)), look((-3.0 * b - std::sqrt(d)) / (10.0 * c));
-        const double t = -b / (2.0 * c);
-        if (t > 0.0 && t < T) factor = std::fmax(factor, even(t));
-    } else if (b != 0.0) {
-        look(-a / (3.0 * b));
-    }
-    const double sy = ortho_scale(S), sa = ortho_scale(T), sc = ortho_scale(std::fabs(c) * T), sf = ortho_scale(factor);
-    S = std::fmax(most, 1e-15);
-    const double sn = ortho_scale(S);
-    OrthoScales s;
-    s.gram = (float)(sa / (sy * sy));
-    s.square = (float)(c * sc / sa);
-    s.linear = (float)(b * sc);
-    s.unit = (float)(a * sa * sc);
-    s.factor = (float)(sf / (sa * sc));
-    s.direct_linear = (float)(b * sf / (sy * sy));
-    s.direct_unit = (float)(a * sf);
-    s.apply = (float)(sn / (sf * sy));
-    s.out = (float)(1.0 / sn);
-    return s;
-}
-
-// Whether the bounds of the singular values are near enough to them for scales that they give.
+// Whether every step's bounds are near enough to what it makes for scales that they give.
 bool ortho_bounded(int steps, const float *coefs)
 {
     double S = 1.0;
     for (int i = 0; i < steps; ++i) {
         if (std::fabs(coefs[3 * i]) < 0.5) return false;
-        (void)ortho_scales(coefs + 3 * i, S);
+        S = ortho_bounds(coefs[3 * i], coefs[3 * i + 1], coefs[3 * i + 2], S).next;
         if (!(S <= 16.0)) return false;
     }
     return true;
 }
 
-// the inverse norms of x's matrices, behind their parts in `sums`
+// What stands behind the matrices in the workspace.
+struct OrthoSums {
+    double *parts, *inverse, *norms;
+    OrthoScales *scales;
+    OrthoSums(uint8_t *ws, int64_t batch, const OrthoPlan &p)
+        : parts(reinterpret_cast<double *>(ws + p.y + 2 * p.yt + 2 * p.f)), inverse(parts + batch * p.parts), norms(inverse + batch),
+          scales(reinterpret_cast<OrthoScales *>(norms + batch)) {}
+};
+
+// the inverse norms of x's matrices, and their norms after that
 template <Type T>
-int ortho_norms(const void *x, int64_t batch, int64_t size, int parts, float eps, double *sums, hipStream_t st)
+int ortho_norms(const void *x, int64_t batch, int64_t size, int chunks, float eps, const OrthoSums &sums, hipStream_t st)
 {
-    if (int rc = check_blocks(batch * parts)) return rc;
-    ortho_norm_kernel<T><<<dim3((unsigned)(batch * parts)), dim3(256), 0, st>>>(x, size, parts, sums);
+    if (int rc = check_blocks(batch * chunks)) return rc;
+    ortho_norm_kernel<T><<<dim3((unsigned)(batch * chunks)), dim3(256), 0, st>>>(x, size, chunks, sums.parts);
     LAUNCHCHK("ortho_norm_kernel");
-    ortho_inverse_kernel<<<dim3((unsigned)batch), dim3(64), 0, st>>>(sums, parts, eps, sums + batch * parts);
+    ortho_inverse_kernel<<<dim3((unsigned)batch), dim3(64), 0, st>>>(sums.parts, chunks, eps, sums.inverse, sums.norms);
     LAUNCHCHK("ortho_inverse_kernel");
     return IVF_OK;
 }
@@ -279,9 +250,9 @@ int ortho_general(const void *x, int64_t batch, int rows, int cols, int steps, c
     // (as many bytes an element as two terms have)
     float *y = reinterpret_cast<float *>(ws), *yt = reinterpret_cast<float *>(ws + p.y), *yt2 = reinterpret_cast<float *>(ws + p.y + p.yt);
     float *a = reinterpret_cast<float *>(ws + p.y + 2 * p.yt), *f = reinterpret_cast<float *>(ws + p.y + 2 * p.yt + p.f);
-    double *sums = reinterpret_cast<double *>(ws + p.y + 2 * p.yt + 2 * p.f);
-    if (int rc = ortho_norms<T>(x, batch, (int64_t)rows * cols, p.parts, eps, sums, st)) return rc;
-    ortho_first_general_kernel<T><<<dim3(4096), dim3(256), 0, st>>>(x, batch, rows, cols, sums + batch * p.parts, turned ? yt : y, turned ? y : yt);
+    const OrthoSums sums(ws, batch, p);
+    if (int rc = ortho_norms<T>(x, batch, (int64_t)rows * cols, p.chunks, eps, sums, st)) return rc;
+    ortho_first_general_kernel<T><<<dim3(4096), dim3(256), 0, st>>>(x, batch, rows, cols, sums.inverse, turned ? yt : y, turned ? y : yt);
     LAUNCHCHK("ortho_first_general_kernel");
     auto product = [&](const OrthoGeneral &g) -> int {
         const int64_t blocks = batch * ceil_div(g.rows_p, 64) * ceil_div(g.rows_q, 64);
@@ -310,26 +281,28 @@ int ortho_steps(const void *x, int64_t batch, int rows, int cols, int steps, con
     OrthoMatrix yt2{reinterpret_cast<uint16_t *>(ws + p.y + p.yt), p.n, p.m, p.ldm};
     OrthoMatrix a{reinterpret_cast<uint16_t *>(ws + p.y + 2 * p.yt), p.m, p.m, p.ldm};
     OrthoMatrix f{reinterpret_cast<uint16_t *>(ws + p.y + 2 * p.yt + p.f), p.m, p.m, p.ldm};
-    double *sums = reinterpret_cast<double *>(ws + p.y + 2 * p.yt + 2 * p.f);
-    const int64_t side = ceil_div(p.m, BS), sym = batch * side * (side + 1) / 2, all = batch * ceil_div(p.m, B) * ceil_div(p.n, B);
+    const OrthoSums sums(ws, batch, p);
+    const int64_t side = ceil_div(p.m, BS), sym = batch * side * (side + 1) / 2, tiles = ceil_div(p.m, B) * ceil_div(p.n, B), all = batch * tiles;
     const int64_t first = batch * ceil_div(rows, 32) * ceil_div(cols, 32);
     if (int rc = check_blocks(std::max(first, std::max(all, sym)))) return rc;
     constexpr unsigned NT = 256;
-    double S = 1.0;
-    if (int rc = ortho_norms<T>(x, batch, (int64_t)rows * cols, p.parts, eps, sums, st)) return rc;
-    ortho_first_kernel<T><<<dim3((unsigned)first), dim3(256), 0, st>>>(x, rows, cols, sums + batch * p.parts, (float)ortho_scale(S), turned ? yt : y, turned ? y : yt);
+    if (int rc = ortho_norms<T>(x, batch, (int64_t)rows * cols, p.chunks, eps, sums, st)) return rc;
+    ortho_first_kernel<T><<<dim3((unsigned)first), dim3(256), 0, st>>>(x, rows, cols, sums.inverse, sums.norms, turned ? yt : y, turned ? y : yt);
     LAUNCHCHK("ortho_first_kernel");
+    double most = 1.0;
     for (int s = 0; s < steps; ++s) {
-        const int direct = coefs[3 * s + 2] == 0.f;
-        const OrthoScales sc = ortho_scales(coefs + 3 * s, S);
-        ortho_symmetric_kernel<BS, 2, true><<<dim3((unsigned)sym), dim3(NT), 0, st>>>(y, direct ? f : a, sc, direct);
+        const float *c = coefs + 3 * s;
+        const int direct = c[2] == 0.f;
+        ortho_scales_kernel<<<dim3((unsigned)batch), dim3(64), 0, st>>>(s ? sums.parts : nullptr, (int)tiles, sums.norms, c[0], c[1], c[2], most, sums.scales);
+        LAUNCHCHK("ortho_scales_kernel");
+        most = ortho_bounds(c[0], c[1], c[2], most).next;
+        ortho_symmetric_kernel<BS, 2, true><<<dim3((unsigned)sym), dim3(NT), 0, st>>>(y, direct ? f : a, sums.scales, direct);
         LAUNCHCHK("ortho_symmetric_kernel");
         if (!direct) {
-            ortho_symmetric_kernel<BS, 2, false><<<dim3((unsigned)sym), dim3(NT), 0, st>>>(a, f, sc, 0);
+            ortho_symmetric_kernel<BS, 2, false><<<dim3((unsigned)sym), dim3(NT), 0, st>>>(a, f, sums.scales, 0);
             LAUNCHCHK("ortho_symmetric_kernel");
         }
-        const bool last = s + 1 == steps;
-        ortho_apply_kernel<B, 2><<<dim3((unsigned)all), dim3(NT), 0, st>>>(yt, f, y, yt2, last ? sc.apply * sc.out : sc.apply, last ? out : nullptr, T, turned);
+        ortho_apply_kernel<B, 2><<<dim3((unsigned)all), dim3(NT), 0, st>>>(yt, f, y, yt2, sums.scales, sums.parts, s + 1 == steps ? out : nullptr, T, turned);
         LAUNCHCHK("ortho_apply_kernel");
         std::swap(yt, yt2);
     }

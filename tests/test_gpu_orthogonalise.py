@@ -61,6 +61,7 @@ LONG = {"no_linear_growth": [(0.5, 0.0, 1e-3)] * 24, "tiny_last": [(0.5, 0.0, 1e
         "only_last": [(0.0, 0.0, 1.0)] * 2, "sign": [(-0.7, 0.2, 0.1)] * 50, "more_than_an_argument": [(0.9, 0.05, 0.01)] * 300,
         "grow": [(1.5, 0.3, 0.2)] * 3}
 SMALL = [(2, 40, 24), (3, 96, 96), (1, 1, 1), (2, 128, 70)]
+LARGE = [(1, 60, 200), (2, 200, 140), (1, 257, 300)]
 
 
 @pytest.mark.parametrize("coefs", LONG, ids=list(LONG))
@@ -120,3 +121,44 @@ def test_small_matrices_as_accurate_as_32_bits(kind, shape):
     got, same = ivf.ivf_orthogonalise(x.cuda(), coefs).double().cpu() - ref, plain(x.cuda(), coefs).double().cpu() - ref
     print("error", got.norm().item(), "in fp32", same.norm().item(), flush=True)
     assert got.norm() <= 1.2 * same.norm()
+
+
+@pytest.mark.parametrize("coefs", LONG, ids=list(LONG))
+@pytest.mark.parametrize("shape", LARGE)
+def test_runs_of_steps_on_large_matrices(coefs, shape):
+    print("case:", coefs, shape, flush=True)
+    check(torch.randn(*shape, generator=gen(len(coefs))), LONG[coefs], eps=0.0)
+
+
+@pytest.mark.parametrize("size,eps", [(1e-30, 1e-7), (1e-4, 1.0), (1e-12, 1e-7), (1e20, 1e3)])
+def test_large_matrices_far_below_eps(size, eps):
+    print("case: below eps", size, eps, flush=True)
+    check(torch.randn(2, 150, 233, generator=gen(3)) * size, POLAR[:5], eps=eps)
+    check(torch.randn(1, 300, 136, generator=gen(4)) * size, UPDATE, eps=eps)
+
+
+def test_large_matrices_infinite_or_not_a_number():
+    print("case: infinite", flush=True)
+    for coefs in (POLAR[:3], [(1.5, -0.5, 0.0)] * 2, [(2.0, 0.0, 0.0)], [(0.0, 0.0, 1.0)]):
+        x = torch.randn(4, 130, 40, generator=gen(5))
+        x[1, 3, 4], x[2, 129, 39] = float("inf"), float("nan")
+        got = ivf.ivf_orthogonalise(x.cuda(), coefs).cpu()
+        assert got[[1, 2]].isnan().all() and got[[0, 3]].isfinite().all()
+
+
+# tiles of 64 and of 128 for both kinds of product, more than eight tiles on the shorter side for each, ends inside a tile and inside 32
+TILES = [(1, 129, 129), (2, 150, 1000), (1, 700, 650), (70, 200, 300), (180, 200, 200), (2, 600, 3300), (12, 1100, 1060), (60, 140, 1030)]
+
+
+@pytest.mark.parametrize("dtype", [F32, torch.bfloat16])
+@pytest.mark.parametrize("shape", TILES)
+def test_large_matrices_of_every_tile(shape, dtype):
+    print("case: tiles", shape, dtype, flush=True)
+    b, r, k = shape
+    x = torch.randn(b, r, k, generator=torch.Generator(device="cuda").manual_seed(sum(shape)), device="cuda") / math.sqrt(r * k)
+    check(x, UPDATE[:3], dtype=dtype)
+    out = ivf.ivf_orthogonalise(x, UPDATE[:3])
+    assert torch.equal(out, ivf.ivf_orthogonalise(x, UPDATE[:3]))
+    # rows and columns exchanged: the same steps on the other side
+    turned = ivf.ivf_orthogonalise(x.transpose(1, 2).contiguous(), UPDATE[:3])
+    assert (turned.transpose(1, 2) - out).flatten(1).norm(dim=1).max() <= 1e-4 * out.flatten(1).norm(dim=1).min()
