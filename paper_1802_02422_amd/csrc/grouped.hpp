@@ -93,12 +93,12 @@ struct GroupedArgs {
 // fp32 components in 4096 groups: 143 us, 3.7 TB/s.
 // One workgroup: BX rows of a group by BW columns of the result, W's rows (or columns) as the first operand so that a lane holds four
 // neighbouring columns of a row.
-template <Type T, bool TRANSPOSED, int BX, int BW>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void grouped_product_kernel(GroupedArgs g)
+template <Type T, bool TRANSPOSED, int BX, int BW, bool APART>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(APART && BX == 128 ? 2 : 3))) void grouped_product_kernel(GroupedArgs g)
 {
     using E = Elem<T>;
     constexpr int WB = BX >= 64 ? 2 : 1;
-    using P = Tile<TRANSPOSED ? E::cols : E::rows, E::terms, BW, 4 / WB, E::rows, E::terms, BX, WB, E::step, E::bufs, E::half>;
+    using P = Tile<TRANSPOSED ? E::cols : E::rows, E::terms, BW, 4 / WB, E::rows, E::terms, BX, WB, E::step, E::bufs, E::half, APART>;
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
     const int cols = TRANSPOSED ? g.C : g.R, K = TRANSPOSED ? g.R : g.C;
     const int tiles = (cols + BW - 1) / BW;
@@ -321,10 +321,10 @@ __device__ __forceinline__ void store_gradient(const P &t, const GradientArgs &g
 
 // Both operands by columns.  500 000 rows of 96 fp32 components in 4096 groups: 198 us, bound by the latency of a short group's steps.
 template <Type T, int BR, int BC>
-__global__ __launch_bounds__(256) void grouped_gradient_kernel(GradientArgs g)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void grouped_gradient_kernel(GradientArgs g)
 {
     using E = Elem<T>;
-    using P = Tile<E::cols, E::terms, BC, 2, E::cols, E::terms, BR, 2, E::step, E::bufs, E::half>;
+    using P = Tile<E::cols, E::terms, BC, 2, E::cols, E::terms, BR, 2, E::step, E::bufs, E::half, T == Type::F32>;
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
     const int across = (g.C + BC - 1) / BC, down = (g.R + BR - 1) / BR;
     uint32_t piece, tile;

@@ -341,7 +341,7 @@ struct OrthoGeneral {
 
 __global__ __launch_bounds__(256) void ortho_general_kernel(OrthoGeneral g)
 {
-    using P = Tile<Form::F_ROWS, 3, 64, 2, Form::F_ROWS, 3, 64, 2, 32, 1, false>;
+    using P = Tile<Form::F_ROWS, 3, 64, 2, Form::F_ROWS, 3, 64, 2, 32, 1, false, true>;
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
     const int across = (g.rows_p + 63) / 64, down = (g.rows_q + 63) / 64;
     const int64_t matrix = blockIdx.x / (across * down), size = (int64_t)g.rows_p * g.rows_q;

@@ -7,7 +7,9 @@
 // terms those with i + j < max(terms of a, terms of b) are formed: for two 32-bit operands six of nine, what is left out is below
 // 2^-21 |a_k b_k| each and about 2^-24 on average, an fp32 rounding.  bfloat16 has fp32's range of exponents, so no scale has to be found
 // first (a pass over the rows, and over the columns for a gradient); an fp32 MFMA reaches a sixteenth of the 16-bit rate, six products a
-// sixth.  An infinite 32-bit operand gives NaN (its second term is infinity less infinity), a NaN gives NaN.
+// sixth.  The instructions round their sum, which makes six roundings of it for 16 products where fp32 by itself would have 16: sums of a few hundred products and more are
+// less accurate than plain fp32 by that (1024 products 4.9e-7 of the result, plain 2.9e-7), which all nine products would not change (4.9e-7).  So the five products with a
+// later term, a 128th of the first's size, go into sums of their own (APART), added at the end: 1.9e-7.  An infinite 32-bit operand gives NaN (its second term is infinity less infinity), a NaN gives NaN.
 #pragma once
 #include <type_traits>
 
@@ -407,8 +409,8 @@ __device__ __forceinline__ uint32_t place_of_block(uint32_t block, uint32_t bloc
 }
 
 // What a tile is made of: BA rows of a by BB rows of b, wavefronts as WA x WB of them, BK elements a step, one or two steps' room in LDS (two
-// spare a barrier, one leaves room for more workgroups).
-template <Form FORM_A, int TERMS_A, int BA, int WA, Form FORM_B, int TERMS_B, int BB, int WB, int BK, int BUFS, bool HALF>
+// spare a barrier, one leaves room for more workgroups).  APART: the products of later terms have sums of their own.
+template <Form FORM_A, int TERMS_A, int BA, int WA, Form FORM_B, int TERMS_B, int BB, int WB, int BK, int BUFS, bool HALF, bool APART = false>
 struct Tile {
     static constexpr int NT = WAVE * WA * WB;
     static constexpr int FA = BA / WA / 32, FB = BB / WB / 32;       // accumulators of a wavefront
@@ -420,7 +422,7 @@ struct Tile {
     static constexpr int OUT_HALVES = NT / WAVE * 32 * (32 * FA) * 2;   // what store() needs
     static constexpr int LDS_HALVES = BUFS * STEP > OUT_HALVES ? BUFS * STEP : OUT_HALVES;
 
-    floatx16 acc[FA][FB];
+    floatx16 acc[FA][FB], later[APART ? FA : 1][APART ? FB : 1];
 
     static __device__ __forceinline__ int row_a(int f) { return (int)(threadIdx.x / WAVE) / WB * (FA * 32) + f * 32; }
     static __device__ __forceinline__ int row_b(int f) { return (int)(threadIdx.x / WAVE) % WB * (FB * 32) + f * 32; }
@@ -432,7 +434,10 @@ struct Tile {
 #pragma unroll
             for (int j = 0; j < FB; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+                for (int e = 0; e < 16; ++e) {
+                    acc[i][j][e] = 0.f;
+                    if constexpr (APART) later[i][j][e] = 0.f;
+                }
     }
 
     // rows_a, rows_b: rows that exist; fragments of others are not multiplied
@@ -466,10 +471,12 @@ struct Tile {
                         for (int j = 0; j < FB; ++j) {
                             if (FA * FB > 1 && (there_a <= 32 * i || there_b <= 32 * j)) continue;
                             const wordx4 u = a[t][i], v = b[order - t][j];
+                            floatx16 *sum = &acc[i][j];
+                            if constexpr (APART) sum = order > 0 ? &later[i][j] : sum;
                             if constexpr (HALF)
-                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, u), __builtin_bit_cast(halfx8, v), acc[i][j], 0, 0, 0);
+                                *sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, u), __builtin_bit_cast(halfx8, v), *sum, 0, 0, 0);
                             else
-                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u), __builtin_bit_cast(bf16x8, v), acc[i][j], 0, 0, 0);
+                                *sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u), __builtin_bit_cast(bf16x8, v), *sum, 0, 0, 0);
                         }
                 }
         }
@@ -495,6 +502,16 @@ struct Tile {
             }
             step(buf, buf + LA::LDS_HALVES, sa.rows, sb.rows);
         }
+        if constexpr (APART)
+#pragma unroll
+            for (int i = 0; i < FA; ++i)
+#pragma unroll
+                for (int j = 0; j < FB; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        acc[i][j][e] += later[i][j][e];
+                        later[i][j][e] = 0.f;
+                    }
         __syncthreads();
     }
 
