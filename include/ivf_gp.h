@@ -415,7 +415,8 @@ int ivf_copy_bytes(void *dst, const void *src, int64_t nbytes, void *hip_stream)
  * Element types: IVF_F32, IVF_F16, IVF_BF16; out_type is the operands' type
  * or IVF_F32.  Sums are fp32, and a result is rounded to 16 bits once.  fp32 operands
  * are multiplied as three bfloat16 terms each with six of the nine products,
- * which is as accurate as fp32 multiplication; an infinite fp32 operand gives NaN.
+ * which is as accurate as fp32 multiplication.  Infinities and NaN go through products as in fp32
+ * arithmetic, however many rows there are.
  * Rows may lie apart: ld* is the number of elements from a row to the next.
  * Any sizes and alignments are right; rows of a multiple of 16 bytes on
  * 16-byte boundaries are loaded by whole words and are faster.
@@ -474,6 +475,8 @@ int ivf_orthogonalise(const void *x, int64_t batch, int rows, int cols, int type
  * largest magnitude, and not below 2^-127; elements are the nearest of 0, 0.5,
  * 1, 1.5, 2, 3, 4, 6 times the scale, ties to the even code, no more than 6.  A block with a
  * NaN or an infinity gets s = 255: all of it is NaN.  Elements past D are zeros.
+ * (With s of 253 or 254, which no quantised row has, values of 4 and 6 may lie past fp32: they are expanded as infinite, and
+ * their products are infinite or NaN, or finite where both sides have 4 bits.)
  * ivf_mx4_expand gives the values back ([n][ldo >= D]).
  */
 int ivf_mx4_quantise(const void *x, int64_t ldx, int64_t n, int D, int type, uint8_t *codes, uint8_t *scales, void *hip_stream);

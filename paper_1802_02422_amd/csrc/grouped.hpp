@@ -113,7 +113,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(APART && BX
         Source sx{g.x + p.row * g.ldx * E::bytes, nullptr, g.ldx, 0, p.rows};
         t.product(sw, sx, 0, K, lds);
     }
+    const bool bad = T == Type::F32 && any_nan(t);
     t.store(static_cast<uint8_t *>(g.y) + (p.row * g.ldy + c0) * (g.out == Type::F32 ? 4 : 2), g.ldy, p.rows, cols - c0, g.out, lds);
+    if (bad && p.group < g.G) {
+        const float *x = reinterpret_cast<const float *>(g.x) + p.row * g.ldx, *w = reinterpret_cast<const float *>(g.w) + (int64_t)p.group * g.R * g.C;
+        mend(static_cast<float *>(g.y) + p.row * g.ldy + c0, g.ldy, p.rows, cols - c0 < BW ? cols - c0 : BW, K, [&](int row, int64_t k) { return x[row * g.ldx + k]; },
+             [&](int col, int64_t k) { return TRANSPOSED ? w[k * g.C + c0 + col] : w[(int64_t)(c0 + col) * g.C + k]; });
+    }
 }
 
 // The same for 16-bit rows and matrices whose lines are whole 16-byte words: 8192 rows, 32 matrices of 2048 x 2048 in bfloat16 128 us, 540 TFLOP/s with groups of
@@ -309,6 +315,8 @@ __device__ __forceinline__ void gradient_place(uint32_t tiles, uint32_t &piece, 
     }
 }
 
+__device__ __forceinline__ float *gradient_part(const GradientArgs &g, const Piece &p) { return g.parts + (part_of(p.begin, g.shift) + p.index) * ((int64_t)g.R * g.C); }
+
 template <class P>
 __device__ __forceinline__ void store_gradient(const P &t, const GradientArgs &g, const Piece &p, int r0, int c0, uint16_t *lds)
 {
@@ -316,7 +324,7 @@ __device__ __forceinline__ void store_gradient(const P &t, const GradientArgs &g
     if (p.group_rows <= 1 << g.shift)
         t.store(static_cast<uint8_t *>(g.dw) + (p.group * size + at) * (g.out == Type::F32 ? 4 : 2), g.C, g.R - r0, g.C - c0, g.out, lds);
     else
-        t.store(g.parts + (part_of(p.begin, g.shift) + p.index) * size + at, g.C, g.R - r0, g.C - c0, Type::F32, lds);
+        t.store(gradient_part(g, p) + at, g.C, g.R - r0, g.C - c0, Type::F32, lds);
 }
 
 // Both operands by columns.  500 000 rows of 96 fp32 components in 4096 groups: 198 us, bound by the latency of a short group's steps.
@@ -341,7 +349,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void g
     Source sx{g.x + (p.row * g.ldx + c0) * E::bytes, nullptr, g.ldx, 0, g.C - c0 < BC ? g.C - c0 : BC};
     Source sd{g.dy + (p.row * g.lddy + r0) * E::bytes, nullptr, g.lddy, 0, g.R - r0 < BR ? g.R - r0 : BR};
     t.product(sx, sd, 0, p.rows, lds);
+    const bool bad = T == Type::F32 && any_nan(t);
     store_gradient(t, g, p, r0, c0, lds);
+    if (bad) {
+        const float *dy = reinterpret_cast<const float *>(g.dy) + p.row * g.lddy + r0, *x = reinterpret_cast<const float *>(g.x) + p.row * g.ldx + c0;
+        float *out = p.group_rows <= 1 << g.shift ? static_cast<float *>(g.dw) + p.group * ((int64_t)g.R * g.C) : gradient_part(g, p);
+        mend(out + (int64_t)r0 * g.C + c0, g.C, g.R - r0 < BR ? g.R - r0 : BR, g.C - c0 < BC ? g.C - c0 : BC, p.rows,
+             [&](int row, int64_t k) { return dy[k * g.lddy + row]; }, [&](int col, int64_t k) { return x[k * g.ldx + col]; });
+    }
 }
 
 template <bool HALF, int BR, int BC, int WR, int WC>

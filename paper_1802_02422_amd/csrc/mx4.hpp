@@ -328,7 +328,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void m
         float v[8];
         eight_of<T>(g.a, (i0 + (row < rows ? row : 0)) * g.lda + k, row < rows ? g.D - k : 0, v);
         uint32_t t[TERMS][4];
-        cut<TERMS, 8>(v, t);
+        cut<TERMS, 8, true>(v, t);
 #pragma unroll
         for (int q = 0; q < TERMS; ++q) a[ks][q] = wordx4{t[q][0], t[q][1], t[q][2], t[q][3]};
     }

@@ -9,7 +9,8 @@
 // first (a pass over the rows, and over the columns for a gradient); an fp32 MFMA reaches a sixteenth of the 16-bit rate, six products a
 // sixth.  The instructions round their sum, which makes six roundings of it for 16 products where fp32 by itself would have 16: sums of a few hundred products and more are
 // less accurate than plain fp32 by that (1024 products 4.9e-7 of the result, plain 2.9e-7), which all nine products would not change (4.9e-7).  So the five products with a
-// later term, a 128th of the first's size, go into sums of their own (APART), added at the end: 1.9e-7.  An infinite 32-bit operand gives NaN (its second term is infinity less infinity), a NaN gives NaN.
+// later term, a 128th of the first's size, go into sums of their own (APART), added at the end: 1.9e-7.  Infinite 32-bit operands need care: infinity less infinity is NaN, and infinity times a later
+// term that is zero.  By single terms (4-bit values) they are the first term and nothing else; results of two 32-bit operands that come out as NaN are formed again in fp32 (mend).
 #pragma once
 #include <type_traits>
 
@@ -73,8 +74,9 @@ __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return 
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
 // Terms of N 32-bit values (N even), two a word: the high 16 bits, then those of what is left; the last term rounded to nearest, which for
-// three terms is exact and for two leaves 2^-17.
-template <int TERMS, int N>
+// three terms is exact and for two leaves 2^-17.  INFINITE: of an infinity nothing is left (else infinity less infinity, NaN), so that its products with
+// single terms are what they are in fp32.
+template <int TERMS, int N, bool INFINITE>
 __device__ __forceinline__ void cut(const float (&v)[N], uint32_t (&out)[TERMS][N / 2])
 {
     float x[N];
@@ -89,7 +91,10 @@ __device__ __forceinline__ void cut(const float (&v)[N], uint32_t (&out)[TERMS][
         }
         if (t + 1 < TERMS)
 #pragma unroll
-            for (int j = 0; j < N; ++j) x[j] -= __uint_as_float(__float_as_uint(x[j]) & 0xFFFF0000u);
+            for (int j = 0; j < N; ++j) {
+                const float high = __uint_as_float(__float_as_uint(x[j]) & 0xFFFF0000u);
+                x[j] = INFINITE && t == 0 && x[j] == high ? 0.f : x[j] - high;
+            }
     }
 }
 
@@ -110,8 +115,8 @@ __device__ __forceinline__ float scale_of(uint32_t byte)
     return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7FC00000u : byte << 23);
 }
 
-// Brings ROWS x BK elements of an operand into LDS by NT threads: load() requests them into registers, store() writes them.
-template <Form FORM, int ROWS, int BK, int NT, int TERMS>
+// Brings ROWS x BK elements of an operand into LDS by NT threads: load() requests them into registers, store() writes them.  INFINITE: as cut().
+template <Form FORM, int ROWS, int BK, int NT, int TERMS, bool INFINITE>
 struct Loader {
     static constexpr int CH = BK / 8;
     static constexpr bool HALVES = FORM == Form::H_ROWS || FORM == Form::HALF_ROWS;
@@ -253,7 +258,7 @@ struct Loader {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(v[2 * j + u]);
                     uint32_t t[TERMS][4];
-                    cut<TERMS, 8>(x, t);
+                    cut<TERMS, 8, INFINITE>(x, t);
 #pragma unroll
                     for (int q = 0; q < TERMS; ++q) put(q, r + u, c, wordx4{t[q][0], t[q][1], t[q][2], t[q][3]});
                 }
@@ -265,7 +270,7 @@ struct Loader {
                     else x[j] = __uint_as_float(v[j]);
                 }
                 uint32_t t[TERMS][4];
-                cut<TERMS, 8>(x, t);
+                cut<TERMS, 8, INFINITE>(x, t);
 #pragma unroll
                 for (int q = 0; q < TERMS; ++q) put(q, id / CH, id % CH, wordx4{t[q][0], t[q][1], t[q][2], t[q][3]});
             }
@@ -400,6 +405,36 @@ __device__ __forceinline__ void store_tile(const P &t, void *out, int64_t ld, in
     }
 }
 
+// Whether any element of the workgroup's tile is NaN, for all of its threads.
+template <class P>
+__device__ __forceinline__ bool any_nan(const P &t)
+{
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < P::FA; ++i)
+#pragma unroll
+        for (int j = 0; j < P::FB; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) bad |= t.acc[i][j][e] != t.acc[i][j][e];
+    return __syncthreads_or(bad);
+}
+
+// Elements of a stored tile [rows][cols] that are NaN anew, as the sum of a(row, k) b(col, k) over k < K one after the other in fp32: for tiles with infinities, or with NaN, whose
+// sums end at the first.
+template <class A, class B>
+__device__ void mend(float *out, int64_t ld, int rows, int cols, int64_t K, A a, B b)
+{
+    __syncthreads();                                          // the tile is stored
+    for (int i = threadIdx.x; i < rows * cols; i += blockDim.x) {
+        const int row = i / cols, col = i % cols;
+        float *p = out + row * ld + col;
+        if (*p == *p) continue;
+        float s = 0.f;
+        for (int64_t k = 0; k < K && s == s; ++k) s = fmaf(a(row, k), b(col, k), s);
+        *p = s;
+    }
+}
+
 // Workgroups are dealt to the eight XCDs in turn: the place in a list of which every XCD takes one run, so that
 // neighbours in the list share that XCD's L2.
 __device__ __forceinline__ uint32_t place_of_block(uint32_t block, uint32_t blocks)
@@ -416,8 +451,8 @@ struct Tile {
     static constexpr int FA = BA / WA / 32, FB = BB / WB / 32;       // accumulators of a wavefront
     static constexpr int ROWS_A = BA;
     static constexpr int MOST = TERMS_A > TERMS_B ? TERMS_A : TERMS_B;
-    using LA = Loader<FORM_A, BA, BK, NT, TERMS_A>;
-    using LB = Loader<FORM_B, BB, BK, NT, TERMS_B>;
+    using LA = Loader<FORM_A, BA, BK, NT, TERMS_A, TERMS_B == 1>;
+    using LB = Loader<FORM_B, BB, BK, NT, TERMS_B, TERMS_A == 1>;
     static constexpr int STEP = LA::LDS_HALVES + LB::LDS_HALVES;     // 16-bit words of LDS a step
     static constexpr int OUT_HALVES = NT / WAVE * 32 * (32 * FA) * 2;   // what store() needs
     static constexpr int LDS_HALVES = BUFS * STEP > OUT_HALVES ? BUFS * STEP : OUT_HALVES;
