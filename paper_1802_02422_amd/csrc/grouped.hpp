@@ -87,6 +87,7 @@ struct GroupedArgs {
     void *y;
     int64_t ldy;
     Type out;
+    uint32_t first;            // workgroup of the list that this launch begins with
 };
 
 // Bound by latency where groups are short (a piece's rows and matrix are a few loads): several workgroups a compute unit.  500 000 rows of 96
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(APART && BX
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
     const int cols = TRANSPOSED ? g.C : g.R, K = TRANSPOSED ? g.R : g.C;
     const int tiles = (cols + BW - 1) / BW;
-    const uint32_t place = place_of_block(blockIdx.x, gridDim.x);
+    const uint32_t place = g.first + place_of_block(blockIdx.x, gridDim.x);
     const Piece p = find_piece(g.offsets, g.G, g.n, log2_of(BX), place / tiles);
     if (p.rows == 0) return;
     const int c0 = (int)(place % tiles) * BW;
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(WAVE *WX *WW) void grouped_product_direct_kernel(Gr
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
     const int cols = TRANSPOSED ? g.C : g.R, K = TRANSPOSED ? g.R : g.C;
     const int tiles = (cols + BW - 1) / BW;
-    const uint32_t place = place_of_block(blockIdx.x, gridDim.x);
+    const uint32_t place = g.first + place_of_block(blockIdx.x, gridDim.x);
     int piece, tile;
     tile_of_place(place, pieces, tiles, piece, tile);
     const Piece p = find_piece(g.offsets, g.G, g.n, log2_of(BX), piece);
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(256) void grouped_product_wide_kernel(GroupedArgs g
     constexpr int BX = 256, BW = 256;
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
     const int tiles = (g.R + BW - 1) / BW;
-    const uint32_t place = place_of_block(blockIdx.x, gridDim.x);
+    const uint32_t place = g.first + place_of_block(blockIdx.x, gridDim.x);
     int piece, tile;
     tile_of_place(place, pieces, tiles, piece, tile);
     const Piece p = find_piece(g.offsets, g.G, g.n, log2_of(BX), piece);
@@ -180,7 +181,7 @@ template <Type T>
 __global__ __launch_bounds__(256) void grouped_few_kernel(GroupedArgs g)
 {
     const int lane = threadIdx.x & 63, tiles = (g.R + 4 * FEW_LINES - 1) / (4 * FEW_LINES);
-    const uint32_t place = place_of_block(blockIdx.x, gridDim.x);
+    const uint32_t place = g.first + place_of_block(blockIdx.x, gridDim.x);
     const Piece p = find_piece(g.offsets, g.G, g.n, log2_of(FEW_ROWS), place / tiles);
     const int r0 = (int)(place % tiles) * (4 * FEW_LINES) + __builtin_amdgcn_readfirstlane((int)(threadIdx.x / WAVE)) * FEW_LINES;
     if (p.rows == 0 || r0 >= g.R) return;
@@ -236,7 +237,7 @@ __global__ __launch_bounds__(256) void grouped_few_transposed_kernel(GroupedArgs
 {
     __shared__ float sums[4][FEW_ROWS][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x / WAVE, tiles = (g.C + 63) / 64;
-    const uint32_t place = place_of_block(blockIdx.x, gridDim.x);
+    const uint32_t place = g.first + place_of_block(blockIdx.x, gridDim.x);
     const Piece p = find_piece(g.offsets, g.G, g.n, log2_of(FEW_ROWS), place / tiles);
     if (p.rows == 0) return;
     const int c0 = (int)(place % tiles) * 64, c = c0 + 8 * (lane & 7);
@@ -292,6 +293,7 @@ struct GradientArgs {
     Type out;
     int shift;                 // rows of a piece are 2^shift: the sum of a longer group is taken in pieces
     float *parts;              // their sums
+    uint32_t first;            // as in GroupedArgs
 };
 
 // Where the sums of a group's pieces are kept: groups with more than one piece have more than T rows, and from
@@ -302,14 +304,14 @@ __device__ __forceinline__ int64_t part_of(int begin, int shift) { return 2 * (i
 // 8192 rows together: 114 us where it took an eighth of the pieces, 77 so); single tiles go by pieces.
 __host__ __device__ __forceinline__ uint32_t gradient_tiles(uint32_t tiles) { return tiles < 8 ? tiles : (tiles + 7) / 8 * 8; }
 
-__device__ __forceinline__ void gradient_place(uint32_t tiles, uint32_t &piece, uint32_t &tile)
+__device__ __forceinline__ void gradient_place(uint32_t first, uint32_t tiles, uint32_t &piece, uint32_t &tile)
 {
     if (tiles < 8) {
-        const uint32_t place = place_of_block(blockIdx.x, gridDim.x);
+        const uint32_t place = first + place_of_block(blockIdx.x, gridDim.x);
         piece = place / tiles;
         tile = place % tiles;
     } else {
-        const uint32_t slice = (tiles + 7) / 8, local = blockIdx.x / 8;
+        const uint32_t slice = (tiles + 7) / 8, local = (first + blockIdx.x) / 8;   // (first: a multiple of 8)
         piece = local / slice;
         tile = blockIdx.x % 8 * slice + local % slice;         // (past the last: nothing to do)
     }
@@ -336,7 +338,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void g
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
     const int across = (g.C + BC - 1) / BC, down = (g.R + BR - 1) / BR;
     uint32_t piece, tile;
-    gradient_place((uint32_t)across * down, piece, tile);
+    gradient_place(g.first, (uint32_t)across * down, piece, tile);
     if (tile >= (uint32_t)across * down) return;
     const Piece p = find_piece(g.offsets, g.G, g.n, g.shift, piece);
     // (a group without rows still has its zeros written, by the number that it leaves unused)
@@ -366,7 +368,7 @@ __global__ __launch_bounds__(WAVE *WR *WC) void grouped_gradient_direct_kernel(G
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
     const int across = (g.C + BC - 1) / BC, down = (g.R + BR - 1) / BR;
     uint32_t piece, tile;
-    gradient_place((uint32_t)across * down, piece, tile);
+    gradient_place(g.first, (uint32_t)across * down, piece, tile);
     if (tile >= (uint32_t)across * down) return;
     const Piece p = find_piece(g.offsets, g.G, g.n, g.shift, piece);
     // (a group without rows still has its zeros written, by the number that it leaves unused)

@@ -8,16 +8,16 @@
 namespace ivf {
 
 // Bound by memory: a lane takes eight components (one or two 16-byte words), four lanes a block, whose largest magnitude they share by DPP; codes
-// are written as a 4-byte word a lane, next to each other.  INDEX: 32 bits where they number all lanes (a division is what a lane's place costs).
+// are written as a 4-byte word a lane, next to each other.
 // 10^6 x 96 fp32: 99 us, 4.4 TB/s.
-template <Type T, typename INDEX>
+template <Type T>
 __global__ __launch_bounds__(256) void mx4_quantise_kernel(const void *__restrict__ x, int64_t ldx, int64_t n, int D, uint32_t *__restrict__ codes,
                                                            uint8_t *__restrict__ scales)
 {
     const int blocks = (D + 31) / 32;
-    const INDEX id = (INDEX)blockIdx.x * 256 + threadIdx.x, row = id / (INDEX)(4 * blocks);
-    if ((int64_t)row >= n) return;                             // (four lanes of a block together)
-    const int c0 = (int)(id - row * (INDEX)(4 * blocks)) * 8;
+    const uint32_t id = blockIdx.x * 256 + threadIdx.x, row = id / (uint32_t)(4 * blocks);
+    if (row >= n) return;                                      // (four lanes of a block together)
+    const int c0 = (int)(id - row * (uint32_t)(4 * blocks)) * 8;
     const int64_t at = (int64_t)row * ldx + c0;
     float v[8];
     if (c0 + 8 <= D) {
@@ -51,15 +51,15 @@ __global__ __launch_bounds__(256) void mx4_quantise_kernel(const void *__restric
 }
 
 // A lane writes 16 bytes: four values in 32 bits, eight in 16.  10^6 x 96 to fp32: 85 us, 5.1 TB/s.
-template <bool FLOAT, typename INDEX>
+template <bool FLOAT>
 __global__ __launch_bounds__(256) void mx4_expand_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t n, int blocks, int D,
                                                          void *__restrict__ out, int64_t ldo, Type type)
 {
     constexpr int PER = FLOAT ? 4 : 8;
     const int per = (D + PER - 1) / PER;
-    const INDEX id = (INDEX)blockIdx.x * 256 + threadIdx.x, row = id / (INDEX)per;
-    if ((int64_t)row >= n) return;
-    const int c0 = (int)(id - row * (INDEX)per) * PER;
+    const uint32_t id = blockIdx.x * 256 + threadIdx.x, row = id / (uint32_t)per;
+    if (row >= n) return;
+    const int c0 = (int)(id - row * (uint32_t)per) * PER;
     const uint8_t *p = codes + (int64_t)row * (blocks * 16) + c0 / 2;
     const float by = scale_of(scales[(int64_t)row * blocks + c0 / 32]);
     const uint32_t word = FLOAT ? *reinterpret_cast<const uint16_t *>(p) : *reinterpret_cast<const uint32_t *>(p);
@@ -94,6 +94,7 @@ struct Mx4Args {
     void *out;
     int64_t ldo;
     Type type;
+    uint32_t first;            // workgroup of the list that this launch begins with
 };
 
 typedef int intx8 __attribute__((ext_vector_type(8)));
@@ -228,7 +229,7 @@ __global__ __launch_bounds__(WAVE *WA *WB) void mx4_product_kernel(Mx4Args g)
     __shared__ wordx4 scales[2][BA + BB];
     const int across = (int)((g.n + BB - 1) / BB), down = (int)((g.m + BA - 1) / BA);
     int i, j;
-    tile_of_place(place_of_block(blockIdx.x, gridDim.x), down, across, i, j);
+    tile_of_place(g.first + place_of_block(blockIdx.x, gridDim.x), down, across, i, j);
     const int64_t i0 = (int64_t)i * BA, j0 = (int64_t)j * BB;
     P t;
     t.clear();
@@ -253,6 +254,7 @@ struct Mx4RowsArgs {
     int parts;                 // TRANSPOSED: more than one: their sums go to part_sums
     int64_t part_rows;
     float *part_sums;          // [parts][m][D]
+    uint32_t first;            // as in Mx4Args
 };
 
 template <Type T>
@@ -281,8 +283,9 @@ __global__ __launch_bounds__(256) void mx4_rows_product_kernel(Mx4RowsArgs g, Mx
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
     const int blocks = (g.D + 31) / 32;
     const int64_t cols = TRANSPOSED ? g.D : g.n, across = (cols + BN - 1) / BN, down = (g.m + BM - 1) / BM;
-    const int64_t j0 = (blockIdx.x % across) * BN, i0 = (blockIdx.x / across % down) * BM;
-    const int part = (int)(blockIdx.x / (across * down));
+    const uint32_t place = g.first + blockIdx.x;
+    const int64_t j0 = (place % across) * BN, i0 = (place / across % down) * BM;
+    const int part = (int)(place / (across * down));
     P t;
     t.clear();
     Source sb = EXPANDED ? Source{reinterpret_cast<const uint8_t *>(values.p + j0), nullptr, values.ld, 0, (int)(cols - j0 < BN ? cols - j0 : BN)} : Source{TRANSPOSED ? g.codes + j0 / 2 : g.codes + j0 * blocks * 16, TRANSPOSED ? g.scales + j0 / 32 : g.scales + j0 * blocks, (int64_t)blocks * 16, 0,
@@ -317,7 +320,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void m
     __shared__ __attribute__((aligned(16))) uint16_t values[2][SWEEP_COLS * W];
     __shared__ __attribute__((aligned(16))) float turned[4][32 * 32];
     const int lane = threadIdx.x & 63;
-    const uint32_t down = (uint32_t)((g.m + SWEEP_ROWS - 1) / SWEEP_ROWS), place = place_of_block(blockIdx.x, gridDim.x);
+    const uint32_t down = (uint32_t)((g.m + SWEEP_ROWS - 1) / SWEEP_ROWS), place = g.first + place_of_block(blockIdx.x, gridDim.x);
     const int64_t i0 = (int64_t)(place % down) * SWEEP_ROWS, tiles = (g.n + SWEEP_COLS - 1) / SWEEP_COLS;
     const int64_t first = (int64_t)(place / down) * run, end = first + run < tiles ? first + run : tiles;
     const int rows = (int)(g.m - i0 < SWEEP_ROWS ? g.m - i0 : SWEEP_ROWS), own = __builtin_amdgcn_readfirstlane(SweepTile::row_b(0));
@@ -391,7 +394,7 @@ __global__ __launch_bounds__(WAVE *WM *WN) void mx4_direct_kernel(Mx4RowsArgs g,
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
     const int64_t cols = TRANSPOSED ? g.D : g.n;
     const int across = (int)((cols + BN - 1) / BN), down = (int)((g.m + BM - 1) / BM);
-    const uint32_t place = place_of_block(blockIdx.x, gridDim.x), part = place / ((uint32_t)across * down);
+    const uint32_t place = g.first + place_of_block(blockIdx.x, gridDim.x), part = place / ((uint32_t)across * down);
     int i, j;
     tile_of_place(place % ((uint32_t)across * down), down, across, i, j);
     const int64_t i0 = (int64_t)i * BM, j0 = (int64_t)j * BN;

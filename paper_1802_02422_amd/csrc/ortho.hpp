@@ -74,10 +74,11 @@ struct OrthoMatrix {
 // step keep enough of memory on its way: 16.8 MB of bfloat16 in 6 us.
 constexpr int NORM_CHUNK = 16384;
 template <Type T>
-__global__ __launch_bounds__(256) void ortho_norm_kernel(const void *__restrict__ x, int64_t size, int parts, double *__restrict__ sums)
+__global__ __launch_bounds__(256) void ortho_norm_kernel(uint32_t first, const void *__restrict__ x, int64_t size, int parts, double *__restrict__ sums)
 {
     __shared__ double wave_sums[4];
-    const int64_t matrix = blockIdx.x / parts, a = (int64_t)(blockIdx.x % parts) * NORM_CHUNK, b = a + NORM_CHUNK < size ? a + NORM_CHUNK : size;
+    const uint32_t place = first + blockIdx.x;
+    const int64_t matrix = place / parts, a = (int64_t)(place % parts) * NORM_CHUNK, b = a + NORM_CHUNK < size ? a + NORM_CHUNK : size;
     double s = 0.0;
 #pragma unroll 4
     for (int64_t i = a + 8 * (int)threadIdx.x; i < b; i += 8 * 256) {
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(const void *__restrict_
     for (int o = WAVE / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, WAVE);
     if ((threadIdx.x & 63) == 0) wave_sums[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0) sums[blockIdx.x] = wave_sums[0] + wave_sums[1] + wave_sums[2] + wave_sums[3];
+    if (threadIdx.x == 0) sums[place] = wave_sums[0] + wave_sums[1] + wave_sums[2] + wave_sums[3];
 }
 
 // 1 / (norm + eps); 0 for a matrix of zeros, which stays one whatever eps is; NaN for one with an infinity or a NaN
@@ -115,21 +116,22 @@ __device__ __forceinline__ double ortho_sum(const double *sums, int parts)
 }
 
 // 1 / (norm + eps) of every matrix and its norm after that, a wavefront each.
-__global__ __launch_bounds__(64) void ortho_inverse_kernel(const double *__restrict__ sums, int parts, double eps, double *__restrict__ inverse, double *__restrict__ norms)
+__global__ __launch_bounds__(64) void ortho_inverse_kernel(uint32_t first, const double *__restrict__ sums, int parts, double eps, double *__restrict__ inverse, double *__restrict__ norms)
 {
-    const double s = ortho_sum(sums + (int64_t)blockIdx.x * parts, parts), by = ortho_inverse(s, eps);
+    const int64_t matrix = first + blockIdx.x;
+    const double s = ortho_sum(sums + matrix * parts, parts), by = ortho_inverse(s, eps);
     if (threadIdx.x == 0) {
-        inverse[blockIdx.x] = by;
-        norms[blockIdx.x] = sqrt(s) * by;
+        inverse[matrix] = by;
+        norms[matrix] = sqrt(s) * by;
     }
 }
 
 // The multipliers of every matrix's next step, a wavefront each: of the first one (sums NULL) from norms, of others from the squares of the scaled Y that the last
 // step's workgroups have summed.  most: a bound of its singular values that follows from the coefficients.
-__global__ __launch_bounds__(64) void ortho_scales_kernel(const double *__restrict__ sums, int parts, const double *__restrict__ norms, double a, double b, double c,
+__global__ __launch_bounds__(64) void ortho_scales_kernel(uint32_t first, const double *__restrict__ sums, int parts, const double *__restrict__ norms, double a, double b, double c,
                                                           double most, OrthoScales *__restrict__ scales)
 {
-    const int64_t matrix = blockIdx.x;
+    const int64_t matrix = first + blockIdx.x;
     OrthoScales &s = scales[matrix];
     const double sy = sums ? s.next : ortho_scale(norms[matrix]);
     const double S = fmin(most, sums ? sqrt(ortho_sum(sums + matrix * parts, parts)) / sy : norms[matrix]);
@@ -165,13 +167,14 @@ __device__ __forceinline__ void ortho_cut(const float (&v)[N], uint32_t (&out)[O
 
 // x over its norm, scaled, as terms, in x's orientation (same) and transposed: 32 x 32 elements a workgroup.
 template <Type T>
-__global__ __launch_bounds__(256) void ortho_first_kernel(const void *__restrict__ x, int rows, int cols, const double *__restrict__ inverse,
+__global__ __launch_bounds__(256) void ortho_first_kernel(uint32_t first, const void *__restrict__ x, int rows, int cols, const double *__restrict__ inverse,
                                                           const double *__restrict__ norms, OrthoMatrix same, OrthoMatrix turned)
 {
     __shared__ float tile[32][33];
     const int across = (cols + 31) / 32, down = (rows + 31) / 32;
-    const int64_t matrix = blockIdx.x / (across * down);
-    const int c0 = (int)(blockIdx.x % across) * 32, r0 = (int)(blockIdx.x / across % down) * 32;
+    const uint32_t place = first + blockIdx.x;
+    const int64_t matrix = place / (across * down);
+    const int c0 = (int)(place % across) * 32, r0 = (int)(place / across % down) * 32;
     const double by = ortho_scale(norms[matrix]) * inverse[matrix];
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
 #pragma unroll
@@ -230,12 +233,12 @@ using OrthoTile = DirectTile<false, ORTHO_TERMS, B, W, false, ORTHO_TERMS, B, W,
 // Symmetric results, the tiles on and below the diagonal, each written to both sides.
 //   GRAM: to = Y Y^T, or a I + b Y Y^T (direct)      else: to = a I + b F + c F F, F symmetric
 template <int B, int W, bool GRAM>
-__global__ __launch_bounds__(WAVE *W *W) void ortho_symmetric_kernel(OrthoMatrix from, OrthoMatrix to, const OrthoScales *__restrict__ scales, int direct)
+__global__ __launch_bounds__(WAVE *W *W) void ortho_symmetric_kernel(uint32_t first, OrthoMatrix from, OrthoMatrix to, const OrthoScales *__restrict__ scales, int direct)
 {
     using P = OrthoTile<B, W>;
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
     const int side = (from.rows + B - 1) / B, count = side * (side + 1) / 2;
-    const uint32_t place = place_of_block(blockIdx.x, gridDim.x);
+    const uint32_t place = first + place_of_block(blockIdx.x, gridDim.x);
     const int64_t matrix = place / count;
     int i, j;
     triangle_of_place((int)(place % count), side, i, j);
@@ -265,13 +268,13 @@ __global__ __launch_bounds__(WAVE *W *W) void ortho_symmetric_kernel(OrthoMatrix
 
 // Y <- F Y from Y transposed: both orientations and the sum of the squares of its scaled elements, or the result itself in x's (last).
 template <int B, int W>
-__global__ __launch_bounds__(WAVE *W *W) void ortho_apply_kernel(OrthoMatrix yt, OrthoMatrix f, OrthoMatrix to, OrthoMatrix to_t, const OrthoScales *__restrict__ scales,
+__global__ __launch_bounds__(WAVE *W *W) void ortho_apply_kernel(uint32_t first, OrthoMatrix yt, OrthoMatrix f, OrthoMatrix to, OrthoMatrix to_t, const OrthoScales *__restrict__ scales,
                                                                  double *__restrict__ sums, void *out, Type type, int turned)
 {
     using P = OrthoTile<B, W>;
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
     const int across = (yt.rows + B - 1) / B, down = (f.rows + B - 1) / B;
-    const uint32_t place = place_of_block(blockIdx.x, gridDim.x);
+    const uint32_t place = first + place_of_block(blockIdx.x, gridDim.x);
     const int64_t matrix = place / (across * down);
     int i, j;
     tile_of_place(place % (across * down), down, across, i, j);
@@ -339,13 +342,14 @@ struct OrthoGeneral {
     int turned;
 };
 
-__global__ __launch_bounds__(256) void ortho_general_kernel(OrthoGeneral g)
+__global__ __launch_bounds__(256) void ortho_general_kernel(uint32_t first, OrthoGeneral g)
 {
     using P = Tile<Form::F_ROWS, 3, 64, 2, Form::F_ROWS, 3, 64, 2, 32, 1, false, true>;
     __shared__ __attribute__((aligned(16))) uint16_t lds[P::LDS_HALVES];
     const int across = (g.rows_p + 63) / 64, down = (g.rows_q + 63) / 64;
-    const int64_t matrix = blockIdx.x / (across * down), size = (int64_t)g.rows_p * g.rows_q;
-    const int i0 = (int)(blockIdx.x % across) * 64, j0 = (int)(blockIdx.x / across % down) * 64;
+    const uint32_t place = first + blockIdx.x;
+    const int64_t matrix = place / (across * down), size = (int64_t)g.rows_p * g.rows_q;
+    const int i0 = (int)(place % across) * 64, j0 = (int)(place / across % down) * 64;
     auto source = [&](const float *p, int rows, int row) {
         return Source{reinterpret_cast<const uint8_t *>(p + (matrix * rows + row) * g.K), nullptr, g.K, 0, rows - row < 64 ? rows - row : 64};
     };

@@ -26,6 +26,7 @@ struct OrthoSmallArgs {
     int rows, cols, steps, turned;                            // turned: Y is X transposed
     Type type;
     double eps;
+    uint32_t first;                                           // matrix that this launch begins with
     const float *more;                                        // more steps: where their coefficients are
     float coefs[3 * ORTHO_SMALL_STEPS];
 };
@@ -185,7 +186,7 @@ struct OrthoSmall {
     __device__ __forceinline__ void run(const OrthoSmallArgs &g, uint16_t *lds, double *sums, int *tops)
     {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / WAVE));
-        const int64_t matrix = blockIdx.x, size = (int64_t)g.rows * g.cols;
+        const int64_t matrix = g.first + blockIdx.x, size = (int64_t)g.rows * g.cols;
         const int m = g.turned ? g.cols : g.rows, n = g.turned ? g.rows : g.cols;
         // the largest of what the wavefronts have put into tops
         auto largest = [&]() {

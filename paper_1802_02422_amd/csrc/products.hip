@@ -16,8 +16,6 @@ using namespace ivf;
 
 namespace {
 
-constexpr int64_t MOST_BLOCKS = (1ll << 31) - 1;
-
 bool type_known(int t) { return t == IVF_F32 || t == IVF_F16 || t == IVF_BF16; }
 Type type_of(int t) { return t == IVF_F32 ? Type::F32 : t == IVF_F16 ? Type::F16 : Type::BF16; }
 int bytes_of(int t) { return t == IVF_F32 ? 4 : 2; }
@@ -31,9 +29,16 @@ int check_types(int type, int out_type)
     return IVF_OK;
 }
 
-int check_blocks(int64_t blocks)
+// A launch has less than 2^32 threads.  launch(first, count) for as many of them as `blocks` workgroups take; they number their work from `first` on, a multiple of 8
+// (the XCDs).
+template <class F>
+int in_launches(int64_t blocks, int threads, F launch)
 {
-    return blocks > MOST_BLOCKS ? fail(IVF_EINVAL, "too large for one launch (%lld workgroups)", (long long)blocks) : IVF_OK;
+    if (blocks >= 1ll << 32) return fail(IVF_EINVAL, "too large (%lld workgroups)", (long long)blocks);
+    const int64_t most = ((1ll << 32) - 1) / threads / 8 * 8;
+    for (int64_t first = 0; first < blocks; first += most)
+        if (int rc = launch((uint32_t)first, dim3((unsigned)std::min(most, blocks - first)))) return rc;
+    return IVF_OK;
 }
 
 int check_groups(int64_t n, int64_t G, int R, int C)
@@ -83,26 +88,29 @@ extern "C" int ivf_grouped_product(const void *x, int64_t ldx, int64_t n, const 
     if (ldx < in || ldy < cols) return fail(IVF_EINVAL, "ldx=%lld or ldy=%lld is less than a row", (long long)ldx, (long long)ldy);
     if (!aligned(x, bytes_of(type)) || !aligned(w, bytes_of(type)) || !aligned(y, bytes_of(out_type))) return fail(IVF_EINVAL, "an array is not aligned to its elements");
     if (n == 0) return IVF_OK;
-    const GroupedArgs a{static_cast<const uint8_t *>(x), ldx, static_cast<const uint8_t *>(w), (int)n, (int)G, R, C, offsets, y, ldy, type_of(out_type)};
+    GroupedArgs a{static_cast<const uint8_t *>(x), ldx, static_cast<const uint8_t *>(w), (int)n, (int)G, R, C, offsets, y, ldy, type_of(out_type), 0};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     return by_type(type, [&](auto t) -> int {
         constexpr Type T = decltype(t)::value;
         auto launch = [&](auto kernel, int BX, int BW) -> int {
-            const int64_t blocks = (n / BX + G + 1) * ceil_div(cols, BW);
-            if (int r2 = check_blocks(blocks)) return r2;
-            kernel<<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a);
-            LAUNCHCHK("grouped_product_kernel");
-            return IVF_OK;
+            return in_launches((n / BX + G + 1) * ceil_div(cols, BW), 256, [&](uint32_t first, dim3 grid) -> int {
+                a.first = first;
+                kernel<<<grid, dim3(256), 0, st>>>(a);
+                LAUNCHCHK("grouped_product_kernel");
+                return IVF_OK;
+            });
         };
         if constexpr (T != Type::F32) {
             constexpr bool HALF = T == Type::F16;
             if (n / G >= 64 && direct_rows(x, ldx, in, type) && direct_rows(w, C, C, type)) {
                 auto direct = [&](auto kernel, int BX, int BW, int threads) -> int {
-                    const int64_t pieces = n / BX + G + 1, blocks = pieces * ceil_div(cols, BW);
-                    if (int r2 = check_blocks(blocks)) return r2;
-                    kernel<<<dim3((unsigned)blocks), dim3((unsigned)threads), 0, st>>>(a, (int)pieces);
-                    LAUNCHCHK("grouped_product_direct_kernel");
-                    return IVF_OK;
+                    const int64_t pieces = n / BX + G + 1;
+                    return in_launches(pieces * ceil_div(cols, BW), threads, [&](uint32_t first, dim3 grid) -> int {
+                        a.first = first;
+                        kernel<<<grid, dim3((unsigned)threads), 0, st>>>(a, (int)pieces);
+                        LAUNCHCHK("grouped_product_direct_kernel");
+                        return IVF_OK;
+                    });
                 };
                 // Tiles of 256 x 256 fill the units with half as many and leave more of the last ones empty, and their first loads and stores are hidden by nothing,
                 // so: long sums, large groups, half the units at least.  Against the others: 2048 rows, 4 matrices of 4096 x 2048 56 us to 63, 16 384 rows and 32 of
@@ -115,14 +123,7 @@ extern "C" int ivf_grouped_product(const void *x, int64_t ldx, int64_t n, const 
                                   : direct(grouped_product_direct_kernel<HALF, false, 128, 256, 2, 4, 32, 3>, 128, 256, 512);
             }
         }
-        if (ceil_div(n, G) <= FEW_ROWS) {
-            const int64_t blocks = (n / FEW_ROWS + G + 1) * ceil_div(cols, transposed ? 64 : 4 * FEW_LINES);
-            if (int r2 = check_blocks(blocks)) return r2;
-            if (transposed) grouped_few_transposed_kernel<T><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a);
-            else grouped_few_kernel<T><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a);
-            LAUNCHCHK("grouped_few_kernel");
-            return IVF_OK;
-        }
+        if (ceil_div(n, G) <= FEW_ROWS) return transposed ? launch(grouped_few_transposed_kernel<T>, FEW_ROWS, 64) : launch(grouped_few_kernel<T>, FEW_ROWS, 4 * FEW_LINES);
         // Rows of a tile by the average group: a last piece is half empty on average, and the smaller tile leaves room for a fourth workgroup on a
         // compute unit (500 000 x 96 fp32 in 4096 groups: 173 us with 64 rows, 318 with 128).  Sums of up to 128 products in fp32 need no sums apart (96 products: 1.5e-7 of
         // the result in 143 us, plain fp32 1.8e-7; 0.8e-7 in 160 us with them).
@@ -160,23 +161,23 @@ extern "C" int ivf_grouped_gradient(const void *dy, int64_t lddy, const void *x,
     if (need > 0 && !aligned(workspace, 16)) return fail(IVF_EINVAL, "workspace must be 16-byte aligned");
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const int shift = gradient_shift(n, G, R, C);
-    const GradientArgs a{static_cast<const uint8_t *>(dy), lddy, static_cast<const uint8_t *>(x), ldx, (int)n, (int)G, R, C, offsets, dw, type_of(out_type),
-                         shift, static_cast<float *>(workspace)};
+    GradientArgs a{static_cast<const uint8_t *>(dy), lddy, static_cast<const uint8_t *>(x), ldx, (int)n, (int)G, R, C, offsets, dw, type_of(out_type),
+                   shift, static_cast<float *>(workspace), 0};
     const int64_t pieces = (n >> shift) + G + 1, blocks = pieces * gradient_tiles((uint32_t)(ceil_div(R, 128) * ceil_div(C, 128)));
-    rc = check_blocks(blocks);
-    if (!rc)
-        rc = by_type(type, [&](auto t) -> int {
-            constexpr Type E = decltype(t)::value;
-            if constexpr (E != Type::F32)
-                if (direct_rows(x, ldx, C, type) && direct_rows(dy, lddy, R, type)) {
-                    grouped_gradient_direct_kernel<E == Type::F16, 128, 128, 2, 2><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a);
-                    LAUNCHCHK("grouped_gradient_direct_kernel");
-                    return IVF_OK;
-                }
-            grouped_gradient_kernel<decltype(t)::value, 128, 128><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a);
-            LAUNCHCHK("grouped_gradient_kernel");
-            return IVF_OK;
-        });
+    rc = by_type(type, [&](auto t) -> int {
+        constexpr Type E = decltype(t)::value;
+        auto launch = [&](auto kernel) -> int {
+            return in_launches(blocks, 256, [&](uint32_t first, dim3 grid) -> int {
+                a.first = first;
+                kernel<<<grid, dim3(256), 0, st>>>(a);
+                LAUNCHCHK("grouped_gradient_kernel");
+                return IVF_OK;
+            });
+        };
+        if constexpr (E != Type::F32)
+            if (direct_rows(x, ldx, C, type) && direct_rows(dy, lddy, R, type)) return launch(grouped_gradient_direct_kernel<E == Type::F16, 128, 128, 2, 2>);
+        return launch(grouped_gradient_kernel<E, 128, 128>);
+    });
     if (rc || need == 0) return rc;
     // (few groups have several pieces: workgroups look at many)
     const int64_t down = std::min<int64_t>(G, 1024), across = std::max<int64_t>(1, std::min(ceil_div((int64_t)R * C, 1024), 4096 / down));
@@ -241,12 +242,17 @@ struct OrthoSums {
 template <Type T>
 int ortho_norms(const void *x, int64_t batch, int64_t size, int chunks, float eps, const OrthoSums &sums, hipStream_t st)
 {
-    if (int rc = check_blocks(batch * chunks)) return rc;
-    ortho_norm_kernel<T><<<dim3((unsigned)(batch * chunks)), dim3(256), 0, st>>>(x, size, chunks, sums.parts);
-    LAUNCHCHK("ortho_norm_kernel");
-    ortho_inverse_kernel<<<dim3((unsigned)batch), dim3(64), 0, st>>>(sums.parts, chunks, eps, sums.inverse, sums.norms);
-    LAUNCHCHK("ortho_inverse_kernel");
-    return IVF_OK;
+    int rc = in_launches(batch * chunks, 256, [&](uint32_t first, dim3 grid) -> int {
+        ortho_norm_kernel<T><<<grid, dim3(256), 0, st>>>(first, x, size, chunks, sums.parts);
+        LAUNCHCHK("ortho_norm_kernel");
+        return IVF_OK;
+    });
+    if (rc) return rc;
+    return in_launches(batch, 64, [&](uint32_t first, dim3 grid) -> int {
+        ortho_inverse_kernel<<<grid, dim3(64), 0, st>>>(first, sums.parts, chunks, eps, sums.inverse, sums.norms);
+        LAUNCHCHK("ortho_inverse_kernel");
+        return IVF_OK;
+    });
 }
 
 template <Type T>
@@ -262,11 +268,11 @@ int ortho_general(const void *x, int64_t batch, int rows, int cols, int steps, c
     ortho_first_general_kernel<T><<<dim3(4096), dim3(256), 0, st>>>(x, batch, rows, cols, sums.inverse, turned ? yt : y, turned ? y : yt);
     LAUNCHCHK("ortho_first_general_kernel");
     auto product = [&](const OrthoGeneral &g) -> int {
-        const int64_t blocks = batch * ceil_div(g.rows_p, 64) * ceil_div(g.rows_q, 64);
-        if (int rc = check_blocks(blocks)) return rc;
-        ortho_general_kernel<<<dim3((unsigned)blocks), dim3(256), 0, st>>>(g);
-        LAUNCHCHK("ortho_general_kernel");
-        return IVF_OK;
+        return in_launches(batch * ceil_div(g.rows_p, 64) * ceil_div(g.rows_q, 64), 256, [&](uint32_t first, dim3 grid) -> int {
+            ortho_general_kernel<<<grid, dim3(256), 0, st>>>(first, g);
+            LAUNCHCHK("ortho_general_kernel");
+            return IVF_OK;
+        });
     };
     for (int s = 0; s < steps; ++s) {
         const float *c = coefs + 3 * s;
@@ -290,41 +296,58 @@ int ortho_steps(const void *x, int64_t batch, int rows, int cols, int steps, con
     OrthoMatrix f{reinterpret_cast<uint16_t *>(ws + p.y + 2 * p.yt + p.f), p.m, p.m, p.ldm};
     const OrthoSums sums(ws, batch, p);
     const int64_t side = ceil_div(p.m, BS), sym = batch * side * (side + 1) / 2, tiles = ceil_div(p.m, B) * ceil_div(p.n, B), all = batch * tiles;
-    const int64_t first = batch * ceil_div(rows, 32) * ceil_div(cols, 32);
-    if (int rc = check_blocks(std::max(first, std::max(all, sym)))) return rc;
-    constexpr unsigned NT = 256;
+    constexpr int NT = 256;
     if (int rc = ortho_norms<T>(x, batch, (int64_t)rows * cols, p.chunks, eps, sums, st)) return rc;
-    ortho_first_kernel<T><<<dim3((unsigned)first), dim3(256), 0, st>>>(x, rows, cols, sums.inverse, sums.norms, turned ? yt : y, turned ? y : yt);
-    LAUNCHCHK("ortho_first_kernel");
+    int rc = in_launches(batch * ceil_div(rows, 32) * ceil_div(cols, 32), NT, [&](uint32_t first, dim3 grid) -> int {
+        ortho_first_kernel<T><<<grid, dim3(NT), 0, st>>>(first, x, rows, cols, sums.inverse, sums.norms, turned ? yt : y, turned ? y : yt);
+        LAUNCHCHK("ortho_first_kernel");
+        return IVF_OK;
+    });
     double most = 1.0;
-    for (int s = 0; s < steps; ++s) {
+    for (int s = 0; s < steps && !rc; ++s) {
         const float *c = coefs + 3 * s;
         const int direct = c[2] == 0.f;
-        ortho_scales_kernel<<<dim3((unsigned)batch), dim3(64), 0, st>>>(s ? sums.parts : nullptr, (int)tiles, sums.norms, c[0], c[1], c[2], most, sums.scales);
-        LAUNCHCHK("ortho_scales_kernel");
+        rc = in_launches(batch, 64, [&](uint32_t first, dim3 grid) -> int {
+            ortho_scales_kernel<<<grid, dim3(64), 0, st>>>(first, s ? sums.parts : nullptr, (int)tiles, sums.norms, c[0], c[1], c[2], most, sums.scales);
+            LAUNCHCHK("ortho_scales_kernel");
+            return IVF_OK;
+        });
         most = ortho_bounds(c[0], c[1], c[2], most).next;
-        ortho_symmetric_kernel<BS, 2, true><<<dim3((unsigned)sym), dim3(NT), 0, st>>>(y, direct ? f : a, sums.scales, direct);
-        LAUNCHCHK("ortho_symmetric_kernel");
-        if (!direct) {
-            ortho_symmetric_kernel<BS, 2, false><<<dim3((unsigned)sym), dim3(NT), 0, st>>>(a, f, sums.scales, 0);
-            LAUNCHCHK("ortho_symmetric_kernel");
-        }
-        ortho_apply_kernel<B, 2><<<dim3((unsigned)all), dim3(NT), 0, st>>>(yt, f, y, yt2, sums.scales, sums.parts, s + 1 == steps ? out : nullptr, T, turned);
-        LAUNCHCHK("ortho_apply_kernel");
+        if (!rc)
+            rc = in_launches(sym, NT, [&](uint32_t first, dim3 grid) -> int {
+                ortho_symmetric_kernel<BS, 2, true><<<grid, dim3(NT), 0, st>>>(first, y, direct ? f : a, sums.scales, direct);
+                LAUNCHCHK("ortho_symmetric_kernel");
+                return IVF_OK;
+            });
+        if (!rc && !direct)
+            rc = in_launches(sym, NT, [&](uint32_t first, dim3 grid) -> int {
+                ortho_symmetric_kernel<BS, 2, false><<<grid, dim3(NT), 0, st>>>(first, a, f, sums.scales, 0);
+                LAUNCHCHK("ortho_symmetric_kernel");
+                return IVF_OK;
+            });
+        if (!rc)
+            rc = in_launches(all, NT, [&](uint32_t first, dim3 grid) -> int {
+                ortho_apply_kernel<B, 2><<<grid, dim3(NT), 0, st>>>(first, yt, f, y, yt2, sums.scales, sums.parts, s + 1 == steps ? out : nullptr, T, turned);
+                LAUNCHCHK("ortho_apply_kernel");
+                return IVF_OK;
+            });
         std::swap(yt, yt2);
     }
-    return IVF_OK;
+    return rc;
 }
 
 template <int MB, int NB>
-int ortho_small(const OrthoSmallArgs &a, int64_t batch, hipStream_t st)
+int ortho_small(OrthoSmallArgs &a, int64_t batch, hipStream_t st)
 {
-    ortho_small_kernel<MB, NB><<<dim3((unsigned)batch), dim3(WAVE * MB), 0, st>>>(a);
-    LAUNCHCHK("ortho_small_kernel");
-    return IVF_OK;
+    return in_launches(batch, WAVE * MB, [&](uint32_t first, dim3 grid) -> int {
+        a.first = first;
+        ortho_small_kernel<MB, NB><<<grid, dim3(WAVE * MB), 0, st>>>(a);
+        LAUNCHCHK("ortho_small_kernel");
+        return IVF_OK;
+    });
 }
 
-int ortho_small(const OrthoSmallArgs &a, int64_t batch, hipStream_t st)
+int ortho_small(OrthoSmallArgs &a, int64_t batch, hipStream_t st)
 {
     const int m = a.turned ? a.cols : a.rows, n = a.turned ? a.rows : a.cols;
     switch ((m + 31) / 32 * 10 + (n + 31) / 32) {
@@ -367,7 +390,7 @@ extern "C" int ivf_orthogonalise(const void *x, int64_t batch, int rows, int col
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     if (rows <= ORTHO_SMALL_SIDE && cols <= ORTHO_SMALL_SIDE) {
-        OrthoSmallArgs a{x, out, rows, cols, steps, rows > cols, type_of(type), eps, nullptr, {}};
+        OrthoSmallArgs a{x, out, rows, cols, steps, rows > cols, type_of(type), eps, 0, nullptr, {}};
         if (steps <= ORTHO_SMALL_STEPS) {
             std::copy(coefs, coefs + 3 * steps, a.coefs);
         } else {
@@ -407,19 +430,32 @@ int check_mx4(const void *codes, const void *scales, int64_t n, int D)
     return IVF_OK;
 }
 
+// launch(first row, rows, grid) for as many launches as rows of `lanes` lanes take, which are numbered in 32 bits
+template <class F>
+int rows_in_launches(int64_t n, int64_t lanes, F launch)
+{
+    const int64_t most = ((1ll << 32) - 256) / lanes;
+    for (int64_t first = 0; first < n; first += most) {
+        const int64_t rows = std::min(most, n - first);
+        if (int rc = launch(first, rows, dim3((unsigned)ceil_div(rows * lanes, 256)))) return rc;
+    }
+    return IVF_OK;
+}
+
 // the values of rows of D components, `width` (0: D) of each row of out written
 int mx4_expand(const uint8_t *codes, const uint8_t *scales, int64_t n, int D, void *out, int64_t ldo, int out_type, hipStream_t st, int width = 0)
 {
-    const int blocks_of_row = (int)ceil_div(D, 32);
+    const int64_t blocks = ceil_div(D, 32);
     if (width) D = width;                                     // (no more than the blocks hold)
     const bool f32 = out_type == IVF_F32;
-    const int64_t lanes = n * ceil_div(D, f32 ? 4 : 8), blocks = ceil_div(lanes, 256);
-    if (int rc = check_blocks(blocks)) return rc;
-    auto go = [&](auto kernel) { kernel<<<dim3((unsigned)blocks), dim3(256), 0, st>>>(codes, scales, n, blocks_of_row, D, out, ldo, type_of(out_type)); };
-    if (lanes + 256 < 1ll << 32) f32 ? go(mx4_expand_kernel<true, uint32_t>) : go(mx4_expand_kernel<false, uint32_t>);
-    else f32 ? go(mx4_expand_kernel<true, uint64_t>) : go(mx4_expand_kernel<false, uint64_t>);
-    LAUNCHCHK("mx4_expand_kernel");
-    return IVF_OK;
+    return rows_in_launches(n, ceil_div(D, f32 ? 4 : 8), [&](int64_t first, int64_t rows, dim3 grid) -> int {
+        const uint8_t *c = codes + first * blocks * 16, *s = scales + first * blocks;
+        void *o = static_cast<uint8_t *>(out) + first * ldo * bytes_of(out_type);
+        if (f32) mx4_expand_kernel<true><<<grid, dim3(256), 0, st>>>(c, s, rows, (int)blocks, D, o, ldo, type_of(out_type));
+        else mx4_expand_kernel<false><<<grid, dim3(256), 0, st>>>(c, s, rows, (int)blocks, D, o, ldo, type_of(out_type));
+        LAUNCHCHK("mx4_expand_kernel");
+        return IVF_OK;
+    });
 }
 
 }  // namespace
@@ -432,16 +468,15 @@ extern "C" int ivf_mx4_quantise(const void *x, int64_t ldx, int64_t n, int D, in
     if (ldx < D) return fail(IVF_EINVAL, "ldx=%lld is less than a row", (long long)ldx);
     if (!aligned(x, bytes_of(type))) return fail(IVF_EINVAL, "x is not aligned to its elements");
     if (n == 0) return IVF_OK;
-    const int64_t lanes = n * 4 * ceil_div(D, 32), blocks = ceil_div(lanes, 256);
-    if (int rc = check_blocks(blocks)) return rc;
+    const int64_t blocks = ceil_div(D, 32);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     return by_type(type, [&](auto t) -> int {
-        constexpr Type T = decltype(t)::value;
-        uint32_t *words = reinterpret_cast<uint32_t *>(codes);
-        if (lanes + 256 < 1ll << 32) mx4_quantise_kernel<T, uint32_t><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(x, ldx, n, D, words, scales);
-        else mx4_quantise_kernel<T, uint64_t><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(x, ldx, n, D, words, scales);
-        LAUNCHCHK("mx4_quantise_kernel");
-        return IVF_OK;
+        return rows_in_launches(n, 4 * blocks, [&](int64_t first, int64_t rows, dim3 grid) -> int {
+            mx4_quantise_kernel<decltype(t)::value><<<grid, dim3(256), 0, st>>>(static_cast<const uint8_t *>(x) + first * ldx * bytes_of(type), ldx, rows, D,
+                                                                               reinterpret_cast<uint32_t *>(codes + first * blocks * 16), scales + first * blocks);
+            LAUNCHCHK("mx4_quantise_kernel");
+            return IVF_OK;
+        });
     });
 }
 
@@ -467,13 +502,14 @@ extern "C" int ivf_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, 
     if (ldo < n) return fail(IVF_EINVAL, "ldo=%lld is less than a row", (long long)ldo);
     if (!aligned(out, bytes_of(out_type))) return fail(IVF_EINVAL, "out is not aligned to its elements");
     if (m == 0 || n == 0) return IVF_OK;
-    const Mx4Args g{a_codes, a_scales, m, b_codes, b_scales, n, (int)ceil_div(D, 32), out, ldo, type_of(out_type)};
+    Mx4Args g{a_codes, a_scales, m, b_codes, b_scales, n, (int)ceil_div(D, 32), out, ldo, type_of(out_type), 0};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const int64_t blocks = ceil_div(m, 128) * ceil_div(n, 128);
-    if ((rc = check_blocks(blocks))) return rc;
-    mx4_product_kernel<128, 2, 128, 2><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(g);
-    LAUNCHCHK("mx4_product_kernel");
-    return IVF_OK;
+    return in_launches(ceil_div(m, 128) * ceil_div(n, 128), 256, [&](uint32_t first, dim3 grid) -> int {
+        g.first = first;
+        mx4_product_kernel<128, 2, 128, 2><<<grid, dim3(256), 0, st>>>(g);
+        LAUNCHCHK("mx4_product_kernel");
+        return IVF_OK;
+    });
 }
 
 namespace {
@@ -536,19 +572,20 @@ int mx4_few(const Mx4RowsArgs &g, Type type, hipStream_t st)
 
 namespace {
 
-int mx4_sweep(const Mx4RowsArgs &g, int type, hipStream_t st)
+int mx4_sweep(Mx4RowsArgs &g, int type, hipStream_t st)
 {
     const int64_t down = ceil_div(g.m, SWEEP_ROWS), tiles = ceil_div(g.n, SWEEP_COLS);
     // runs of tiles: three workgroups a compute unit, or more where runs would be long
     const int64_t wanted = std::max<int64_t>(1, 3 * 256 / down), run = std::max<int64_t>(8, std::min<int64_t>(ceil_div(tiles, wanted), 256));
-    const int64_t blocks = down * ceil_div(tiles, run);
-    if (int rc = check_blocks(blocks)) return rc;
     return by_type(type, [&](auto t) -> int {
         constexpr Type T = decltype(t)::value;
         auto go = [&](auto kernel) -> int {
-            kernel<<<dim3((unsigned)blocks), dim3(256), 0, st>>>(g, (int)run);
-            LAUNCHCHK("mx4_sweep_kernel");
-            return IVF_OK;
+            return in_launches(down * ceil_div(tiles, run), 256, [&](uint32_t first, dim3 grid) -> int {
+                g.first = first;
+                kernel<<<grid, dim3(256), 0, st>>>(g, (int)run);
+                LAUNCHCHK("mx4_sweep_kernel");
+                return IVF_OK;
+            });
         };
         switch ((g.D + 31) / 32) {
         case 2: return go(mx4_sweep_kernel<T, 2>);
@@ -586,8 +623,8 @@ extern "C" int ivf_mx4_rows_product(const void *a, int64_t lda, int64_t m, int t
     if (m == 0 || cols == 0) return IVF_OK;
     const RowsPlan p = rows_plan(m, n, D, transposed, type);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
-    const Mx4RowsArgs g{static_cast<const uint8_t *>(a), lda, m, codes, scales, n, D, out, ldo, type_of(out_type), (int)p.parts, p.part_rows,
-                        reinterpret_cast<float *>(ws + p.values)};
+    Mx4RowsArgs g{static_cast<const uint8_t *>(a), lda, m, codes, scales, n, D, out, ldo, type_of(out_type), (int)p.parts, p.part_rows,
+                  reinterpret_cast<float *>(ws + p.values), 0};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (!transposed && mx4_few_fits(m, D)) return mx4_few(g, type_of(type), st);
     // Runs of tiles need work for every compute unit: a run is a chain of eight tiles at least.  Of 96 components in fp32 against single tiles 128 x 65 536 20
@@ -595,11 +632,12 @@ extern "C" int ivf_mx4_rows_product(const void *a, int64_t lda, int64_t m, int t
     if (!transposed && D > 32 && D <= 128 && m >= 64 && n >= 16 * SWEEP_COLS && m >= (int64_t{1} << 24) / n) return mx4_sweep(g, type, st);
     const Mx4Values v{reinterpret_cast<const uint16_t *>(ws), p.ld};
     auto launch = [&](auto kernel, int BM, int BN, unsigned threads) -> int {
-        const int64_t blocks = ceil_div(m, BM) * ceil_div(cols, BN) * p.parts;
-        if (int r2 = check_blocks(blocks)) return r2;
-        kernel<<<dim3((unsigned)blocks), dim3(threads), 0, st>>>(g, v);
-        LAUNCHCHK("mx4_rows_product_kernel");
-        return IVF_OK;
+        return in_launches(ceil_div(m, BM) * ceil_div(cols, BN) * p.parts, (int)threads, [&](uint32_t first, dim3 grid) -> int {
+            g.first = first;
+            kernel<<<grid, dim3(threads), 0, st>>>(g, v);
+            LAUNCHCHK("mx4_rows_product_kernel");
+            return IVF_OK;
+        });
     };
     const bool direct = type == IVF_BF16 && direct_rows(a, lda, in, type);
     if (p.values && (transposed || direct)) {
