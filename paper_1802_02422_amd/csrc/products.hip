@@ -193,6 +193,7 @@ constexpr int ORTHO_MOST_STEPS = 1000;
 struct OrthoPlan {
     int m, n, ldm, ldn, chunks, parts;
     int64_t y, yt, f, sums, total;                            // bytes
+    bool small;
 };
 
 int ortho_plan(int64_t batch, int rows, int cols, int type, OrthoPlan &p)
@@ -213,7 +214,9 @@ int ortho_plan(int64_t batch, int rows, int cols, int type, OrthoPlan &p)
     // sums of squares by chunks of X or by tiles of Y, of 64 x 64 at least; of each matrix an inverse norm, a norm and the multipliers
     p.parts = (int)std::max<int64_t>(p.chunks, ceil_div(p.m, 64) * ceil_div(p.n, 64));
     p.sums = whole(batch * (p.parts * 8 + 16 + (int64_t)sizeof(OrthoScales)));
-    p.total = std::max<int64_t>(p.y + 2 * p.yt + 2 * p.f + p.sums, 3 * ORTHO_MOST_STEPS * sizeof(float));
+    // (matrices that one launch takes through all steps: no more than the coefficients of a long run)
+    p.small = rows <= ORTHO_SMALL_SIDE && cols <= ORTHO_SMALL_SIDE;
+    p.total = p.small ? whole(3 * ORTHO_MOST_STEPS * sizeof(float)) : p.y + 2 * p.yt + 2 * p.f + p.sums;
     return IVF_OK;
 }
 
@@ -389,7 +392,7 @@ extern "C" int ivf_orthogonalise(const void *x, int64_t batch, int rows, int col
     if (!aligned(workspace, 16)) return fail(IVF_EINVAL, "workspace must be 16-byte aligned");
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
-    if (rows <= ORTHO_SMALL_SIDE && cols <= ORTHO_SMALL_SIDE) {
+    if (p.small) {
         OrthoSmallArgs a{x, out, rows, cols, steps, rows > cols, type_of(type), eps, 0, nullptr, {}};
         if (steps <= ORTHO_SMALL_STEPS) {
             std::copy(coefs, coefs + 3 * steps, a.coefs);
