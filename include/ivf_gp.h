@@ -492,7 +492,8 @@ int ivf_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, int64_t m, 
  * against rows kept in 4 bits); with `transposed` out [m][ldo >= D] =
  * a b, a [m][lda >= n]: the gradient to a.  From 256 rows of a on that (and
  * IVF_BF16 rows of 512 components or more) goes through b's values as
- * bfloat16 in the workspace, up to 1 GiB.
+ * bfloat16 in the workspace, up to 1 GiB; without `transposed` only where a's rows are whole 16-byte
+ * words on 16-byte boundaries, and none is asked for else.
  */
 int64_t ivf_mx4_rows_product_workspace(int64_t m, int64_t n, int D, int transposed, int type);
 int ivf_mx4_rows_product(const void *a, int64_t lda, int64_t m, int type, const uint8_t *codes, const uint8_t *scales,

@@ -663,6 +663,8 @@ def ivf_mx4_rows_product(a: torch.Tensor, b: Mx4Rows, transposed: bool = False, 
     ldo, out_kind = _rows(out, "out", shape)
     _same_device(a, codes=b.codes, scales=b.scales, out=out)
     need = lib.ivf_mx4_rows_product_workspace(m, n, D, int(transposed), kind)
+    if not transposed and (a.data_ptr() % 16 or lda % 8):      # (rows that are no whole words need none)
+        need = min(need, 0)
     ws = _workspace(need, a)
     _check(lib.ivf_mx4_rows_product(a.data_ptr(), lda, m, kind, b.codes.data_ptr(), b.scales.data_ptr(), n, D, int(transposed),
                                     out.data_ptr(), ldo, out_kind, _ptr(ws), need, _stream_of(a)))

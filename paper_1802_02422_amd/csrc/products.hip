@@ -517,17 +517,18 @@ extern "C" int ivf_mx4_product(const uint8_t *a_codes, const uint8_t *a_scales, 
 
 namespace {
 
-// How a product of rows with 4-bit rows goes: through b's values (bfloat16, in the workspace) where enough rows of a share them, up to 1 GiB; and
+// How a product of rows with 4-bit rows goes: through b's values (bfloat16, in the workspace) where enough rows of a share them, up to 1 GiB (not transposed only for rows
+// of a that are copied straight into LDS, `words`: others multiply expanded codes faster, 4096 x 8192 x 1024 in 170 us against 250); and
 // in how many parts of how many rows of b the sum over those is taken (TRANSPOSED): as many as make `wanted` workgroups, of no less than 256 rows.
 struct RowsPlan {
     int64_t ld, values, parts, part_rows, sums;               // bytes of the values and of the parts' sums
 };
 
-RowsPlan rows_plan(int64_t m, int64_t n, int D, int transposed, int type)
+RowsPlan rows_plan(int64_t m, int64_t n, int D, int transposed, int type, bool words)
 {
     RowsPlan p{};
     p.ld = ceil_div(D, 8) * 8;
-    if (m >= 256 && n > 0 && (transposed || (type == IVF_BF16 && D >= 512)) && n * p.ld * 2 <= 1ll << 30) p.values = ceil_div(n * p.ld * 2, 256) * 256;
+    if (m >= 256 && n > 0 && (transposed || (words && type == IVF_BF16 && D >= 512)) && n * p.ld * 2 <= 1ll << 30) p.values = ceil_div(n * p.ld * 2, 256) * 256;
     p.parts = 1;
     p.part_rows = n;
     if (!transposed || m == 0 || n == 0) return p;
@@ -604,7 +605,7 @@ extern "C" int64_t ivf_mx4_rows_product_workspace(int64_t m, int64_t n, int D, i
 {
     if (!type_known(type)) return fail(IVF_EINVAL, "type=%d is none of IVF_F32, IVF_F16, IVF_BF16", type);
     if (check_rows_product(m, n, D)) return IVF_EINVAL;
-    const RowsPlan p = rows_plan(m, n, D, transposed, type);
+    const RowsPlan p = rows_plan(m, n, D, transposed, type, D % 8 == 0);
     return p.values + p.sums;
 }
 
@@ -620,11 +621,12 @@ extern "C" int ivf_mx4_rows_product(const void *a, int64_t lda, int64_t m, int t
     if (lda < in || ldo < cols) return fail(IVF_EINVAL, "lda=%lld or ldo=%lld is less than a row", (long long)lda, (long long)ldo);
     if (m > 0 && cols > 0 && (!out || (in > 0 && !a))) return fail(IVF_EINVAL, "NULL argument");
     if (!aligned(a, bytes_of(type)) || !aligned(out, bytes_of(out_type))) return fail(IVF_EINVAL, "an array is not aligned to its elements");
-    const int64_t need = ivf_mx4_rows_product_workspace(m, n, D, transposed, type);
+    const bool direct = type == IVF_BF16 && direct_rows(a, lda, in, type);
+    const RowsPlan p = rows_plan(m, n, D, transposed, type, direct);
+    const int64_t need = p.values + p.sums;
     if (workspace_bytes < need || (need > 0 && !workspace)) return fail(IVF_EINVAL, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
     if (need > 0 && !aligned(workspace, 16)) return fail(IVF_EINVAL, "workspace must be 16-byte aligned");
     if (m == 0 || cols == 0) return IVF_OK;
-    const RowsPlan p = rows_plan(m, n, D, transposed, type);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     Mx4RowsArgs g{static_cast<const uint8_t *>(a), lda, m, codes, scales, n, D, out, ldo, type_of(out_type), (int)p.parts, p.part_rows,
                   reinterpret_cast<float *>(ws + p.values), 0};
@@ -642,8 +644,7 @@ extern "C" int ivf_mx4_rows_product(const void *a, int64_t lda, int64_t m, int t
             return IVF_OK;
         });
     };
-    const bool direct = type == IVF_BF16 && direct_rows(a, lda, in, type);
-    if (p.values && (transposed || direct)) {
+    if (p.values) {
         // (columns up to ld: zeros, as the codes past D are)
         if ((rc = mx4_expand(codes, scales, n, D, ws, p.ld, IVF_BF16, st, (int)p.ld))) return rc;
         if (direct) rc = transposed ? launch(mx4_direct_kernel<true, 128, 128, 2, 2, 64, 2>, 128, 128, 256) : launch(mx4_direct_kernel<false, 128, 256, 2, 4, 32, 3>, 128, 256, 512);

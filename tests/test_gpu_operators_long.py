@@ -92,3 +92,18 @@ def test_products_with_many_rows_in_4_bits():
     a4 = ivf.ivf_mx4_quantise(a[:1])
     got = ivf.ivf_mx4_product(a4, b, out_dtype=BF16)
     assert torch.equal(got[:, some], ivf.ivf_mx4_product(a4, few, out_dtype=BF16))
+
+
+def test_rows_of_no_whole_words_take_no_scratch():
+    """bfloat16 rows at odd places against long 4-bit rows: no room for values that are not expanded for them."""
+    print("case: scratch", flush=True)
+    n, D = 65536, 1024
+    b = ivf.ivf_mx4_quantise(whole(n, D))
+    a = whole(256, D + 8, seed=3)
+    out = torch.empty(256, n, dtype=F32, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    ivf.ivf_mx4_rows_product(a[:, 3:3 + D], b, out=out)
+    assert torch.cuda.max_memory_allocated() == before
+    assert torch.equal(out[:, :50], a[:, 3:3 + D].float() @ ivf.ivf_mx4_expand(b)[:50].t().contiguous())
