@@ -506,6 +506,16 @@ def _result(out: Optional[torch.Tensor], shape, like: torch.Tensor, out_dtype, a
     return out
 
 
+def _tracked(*tensors) -> bool:
+    """Whether autograd follows any of them."""
+    return torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors)
+
+
+def _no_gradient(name: str, *tensors):
+    if _tracked(*tensors):
+        raise IvfError(f"{name} has no gradient: call it under torch.no_grad() or on detached tensors")
+
+
 def _workspace(nbytes: int, like: torch.Tensor):
     if nbytes < 0:
         raise IvfError(f"ivf error {nbytes}: {ivf_last_error()}")
@@ -517,7 +527,16 @@ def ivf_grouped_product(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
     """Rows times their group's matrix: out[i] = w[g] x[i] (``transposed``: w[g]^T x[i]) for offsets[g] <= i < offsets[g + 1].
 
     x [n, C] (transposed: [n, R]), w [G, R, C] of the same type, offsets [G + 1] int32 ascending from 0 (as ``ivf_group`` gives
-    them); rows behind offsets[G] get zeros."""
+    them); rows behind offsets[G] get zeros.  Autograd follows x and w (without ``out``), through ``ivf_grouped_gradient`` and the
+    product the other way round; gradients are formed in the operands' type."""
+    if _tracked(x, w, out):
+        if out is not None:
+            raise IvfError("out cannot be given where gradients are asked for")
+        return _GroupedProduct.apply(x, w, offsets, transposed, out_dtype)
+    return _grouped_product(x, w, offsets, transposed, out, out_dtype)
+
+
+def _grouped_product(x, w, offsets, transposed, out, out_dtype):
     lib = load_library()
     if not isinstance(w, torch.Tensor) or w.dim() != 3:
         raise IvfError("w must be a device tensor [G, R, C]")
@@ -541,7 +560,16 @@ def ivf_grouped_gradient_workspace(n: int, G: int, R: int, cols: int) -> int:
 
 
 def ivf_grouped_gradient(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None, out_dtype=None):
-    """[G, R, C]: the sum of dy[i] x[i]^T over each group's rows, for dy [n, R] and x [n, C] of one type."""
+    """[G, R, C]: the sum of dy[i] x[i]^T over each group's rows, for dy [n, R] and x [n, C] of one type.  Autograd follows both (without
+    ``out``)."""
+    if _tracked(dy, x, out):
+        if out is not None:
+            raise IvfError("out cannot be given where gradients are asked for")
+        return _GroupedGradient.apply(dy, x, offsets, out_dtype)
+    return _grouped_gradient(dy, x, offsets, out, out_dtype)
+
+
+def _grouped_gradient(dy, x, offsets, out, out_dtype):
     lib = load_library()
     if not isinstance(dy, torch.Tensor) or not isinstance(x, torch.Tensor) or dy.dim() != 2 or x.dim() != 2:
         raise IvfError("dy and x must be device tensors [n, R] and [n, C]")
@@ -561,6 +589,36 @@ def ivf_grouped_gradient(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tenso
     return out
 
 
+class _GroupedProduct(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, offsets, transposed, out_dtype):
+        ctx.save_for_backward(x, w, offsets)
+        ctx.transposed = transposed
+        return _grouped_product(x, w, offsets, transposed, None, out_dtype)
+
+    @staticmethod
+    def backward(ctx, g):
+        x, w, offsets = ctx.saved_tensors
+        g = g.to(x.dtype).contiguous()                         # (a sum's gradient is one element, expanded)
+        dx = ivf_grouped_product(g, w, offsets, transposed=not ctx.transposed) if ctx.needs_input_grad[0] else None
+        dw = ivf_grouped_gradient(*((x, g) if ctx.transposed else (g, x)), offsets) if ctx.needs_input_grad[1] else None
+        return dx, dw, None, None, None
+
+
+class _GroupedGradient(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, dy, x, offsets, out_dtype):
+        ctx.save_for_backward(dy, x, offsets)
+        return _grouped_gradient(dy, x, offsets, None, out_dtype)
+
+    @staticmethod
+    def backward(ctx, g):
+        dy, x, offsets = ctx.saved_tensors
+        g = g.to(x.dtype).contiguous()
+        return (ivf_grouped_product(x, g, offsets) if ctx.needs_input_grad[0] else None,
+                ivf_grouped_product(dy, g, offsets, transposed=True) if ctx.needs_input_grad[1] else None, None, None)
+
+
 def ivf_orthogonalise_workspace(batch: int, rows: int, cols: int, dtype=torch.float32) -> int:
     """Bytes of scratch of ``ivf_orthogonalise``."""
     return int(load_library().ivf_orthogonalise_workspace(batch, rows, cols, _TYPES.get(dtype, -1)))
@@ -568,7 +626,8 @@ def ivf_orthogonalise_workspace(batch: int, rows: int, cols: int, dtype=torch.fl
 
 def ivf_orthogonalise(x: torch.Tensor, coefs, eps: float = 1e-7, out: Optional[torch.Tensor] = None):
     """Newton-Schulz steps X <- a X + b A X + c A^2 X, A = X X^T, from X = x / (||x||_F + eps), on every matrix of x [..., rows, cols];
-    ``coefs``: one (a, b, c) a step.  ``out`` may be x."""
+    ``coefs``: one (a, b, c) a step.  ``out`` may be x.  It has no gradient, and refuses tensors that ask for one."""
+    _no_gradient("ivf_orthogonalise", x, out)
     lib = load_library()
     if not isinstance(x, torch.Tensor) or x.dim() < 2 or x.dtype not in _TYPES:
         raise IvfError("x must be a device tensor [..., rows, cols] of float32, float16 or bfloat16")
@@ -606,7 +665,8 @@ class Mx4Rows:
 
 
 def ivf_mx4_quantise(x: torch.Tensor) -> Mx4Rows:
-    """The rows of x [n, D] in microscaled 4-bit floating point."""
+    """The rows of x [n, D] in microscaled 4-bit floating point.  Rounding has no gradient: tensors that ask for one are refused."""
+    _no_gradient("ivf_mx4_quantise", x)
     lib = load_library()
     if not isinstance(x, torch.Tensor) or x.dim() != 2:
         raise IvfError("x must be a device tensor [n, D]")
@@ -651,7 +711,29 @@ def ivf_mx4_rows_product_workspace(m: int, n: int, D: int, transposed: bool = Fa
 
 
 def ivf_mx4_rows_product(a: torch.Tensor, b: Mx4Rows, transposed: bool = False, out: Optional[torch.Tensor] = None, out_dtype=None):
-    """[m, n] = a b^T for rows a [m, D] as they are and b [n, D] in 4 bits, or (``transposed``) [m, D] = a b for a [m, n]."""
+    """[m, n] = a b^T for rows a [m, D] as they are and b [n, D] in 4 bits, or (``transposed``) [m, D] = a b for a [m, n].  Autograd follows a
+    (without ``out``), through the product the other way round."""
+    if _tracked(a, out):
+        if out is not None:
+            raise IvfError("out cannot be given where gradients are asked for")
+        return _Mx4RowsProduct.apply(a, b, transposed, out_dtype)
+    return _mx4_rows_product(a, b, transposed, out, out_dtype)
+
+
+class _Mx4RowsProduct(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, a, b, transposed, out_dtype):
+        ctx.save_for_backward(b.codes, b.scales)
+        ctx.dtype, ctx.D, ctx.transposed = a.dtype, b.D, transposed
+        return _mx4_rows_product(a, b, transposed, None, out_dtype)
+
+    @staticmethod
+    def backward(ctx, g):
+        rows = Mx4Rows(*ctx.saved_tensors, ctx.D)
+        return ivf_mx4_rows_product(g.to(ctx.dtype).contiguous(), rows, transposed=not ctx.transposed), None, None, None
+
+
+def _mx4_rows_product(a, b, transposed, out, out_dtype):
     lib = load_library()
     n = b._check("b")
     if not isinstance(a, torch.Tensor) or a.dim() != 2:
