@@ -499,6 +499,8 @@ def _result(out: Optional[torch.Tensor], shape, like: torch.Tensor, out_dtype, a
         if dtype not in _TYPES:
             raise IvfError(f"out_dtype must be float32, float16 or bfloat16, got {dtype}")
         out = torch.empty(shape, dtype=dtype, device=like.device)
+    elif not isinstance(out, torch.Tensor):
+        raise IvfError("out must be a device tensor")
     elif out_dtype is not None and out.dtype != out_dtype:
         raise IvfError(f"out must be {out_dtype}, got {out.dtype}")
     if not any_type and out.dtype not in (like.dtype, torch.float32):
@@ -540,6 +542,8 @@ def _grouped_product(x, w, offsets, transposed, out, out_dtype):
     lib = load_library()
     if not isinstance(w, torch.Tensor) or w.dim() != 3:
         raise IvfError("w must be a device tensor [G, R, C]")
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise IvfError("x must be a two-dimensional device tensor")
     G, R, Cc = w.shape
     n = x.shape[0]
     ldx, kind = _rows(x, "x", (n, R if transposed else Cc))
@@ -573,6 +577,8 @@ def _grouped_gradient(dy, x, offsets, out, out_dtype):
     lib = load_library()
     if not isinstance(dy, torch.Tensor) or not isinstance(x, torch.Tensor) or dy.dim() != 2 or x.dim() != 2:
         raise IvfError("dy and x must be device tensors [n, R] and [n, C]")
+    if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1:
+        raise IvfError("offsets must be a 32-bit tensor of G + 1 entries")
     n, R = dy.shape
     Cc = x.shape[1]
     G = offsets.shape[0] - 1
@@ -633,7 +639,8 @@ def ivf_orthogonalise(x: torch.Tensor, coefs, eps: float = 1e-7, out: Optional[t
         raise IvfError("x must be a device tensor [..., rows, cols] of float32, float16 or bfloat16")
     _dev(x, x.dtype, "x")
     rows, cols = x.shape[-2:]
-    flat = [float(v) for step in coefs for v in step]
+    coefs = [[float(v) for v in step] for step in coefs]
+    flat = [v for step in coefs for v in step]
     if not flat or any(len(step) != 3 for step in coefs):
         raise IvfError("coefs must hold one (a, b, c) for each step")
     if out is None:
@@ -658,10 +665,18 @@ class Mx4Rows:
     D: int
 
     def _check(self, name: str) -> int:
+        if not all(isinstance(t, torch.Tensor) and t.dim() == 2 for t in (self.codes, self.scales)):
+            raise IvfError(f"{name}: codes and scales must be two-dimensional device tensors")
         n, blocks = self.codes.shape[0], -(-self.D // 32)
         _dev(self.codes, torch.uint8, f"{name}.codes", (n, 16 * blocks))
         _dev(self.scales, torch.uint8, f"{name}.scales", (n, blocks))
         return n
+
+
+def _four_bits(rows: Mx4Rows, name: str) -> int:
+    if not isinstance(rows, Mx4Rows):
+        raise IvfError(f"{name} must be Mx4Rows, as ivf_mx4_quantise gives them")
+    return rows._check(name)
 
 
 def ivf_mx4_quantise(x: torch.Tensor) -> Mx4Rows:
@@ -683,7 +698,7 @@ def ivf_mx4_quantise(x: torch.Tensor) -> Mx4Rows:
 def ivf_mx4_expand(rows: Mx4Rows, out: Optional[torch.Tensor] = None, out_dtype=None):
     """The values [n, D] of 4-bit rows, float32 unless ``out`` or ``out_dtype`` says otherwise."""
     lib = load_library()
-    n = rows._check("rows")
+    n = _four_bits(rows, "rows")
     out = _result(out, (n, rows.D), rows.codes, torch.float32 if out is None and out_dtype is None else out_dtype, any_type=True)
     ldo, kind = _rows(out, "out", (n, rows.D))
     _same_device(rows.codes, scales=rows.scales, out=out)
@@ -694,7 +709,7 @@ def ivf_mx4_expand(rows: Mx4Rows, out: Optional[torch.Tensor] = None, out_dtype=
 def ivf_mx4_product(a: Mx4Rows, b: Mx4Rows, out: Optional[torch.Tensor] = None, out_dtype=None):
     """[m, n] = a b^T of rows in 4 bits, float32 unless ``out`` or ``out_dtype`` says otherwise."""
     lib = load_library()
-    m, n = a._check("a"), b._check("b")
+    m, n = _four_bits(a, "a"), _four_bits(b, "b")
     if a.D != b.D:
         raise IvfError(f"a has {a.D} components, b {b.D}")
     out = _result(out, (m, n), a.codes, torch.float32 if out is None and out_dtype is None else out_dtype, any_type=True)
@@ -735,7 +750,7 @@ class _Mx4RowsProduct(torch.autograd.Function):
 
 def _mx4_rows_product(a, b, transposed, out, out_dtype):
     lib = load_library()
-    n = b._check("b")
+    n = _four_bits(b, "b")
     if not isinstance(a, torch.Tensor) or a.dim() != 2:
         raise IvfError("a must be a two-dimensional device tensor")
     m, D = a.shape[0], b.D

@@ -162,3 +162,16 @@ def test_large_matrices_of_every_tile(shape, dtype):
     # rows and columns exchanged: the same steps on the other side
     turned = ivf.ivf_orthogonalise(x.transpose(1, 2).contiguous(), UPDATE[:3])
     assert (turned.transpose(1, 2) - out).flatten(1).norm(dim=1).max() <= 1e-4 * out.flatten(1).norm(dim=1).min()
+
+
+def test_coefficients_from_a_generator():
+    """Looked at once: a step that is no triple is refused wherever it stands, others give what a list gives."""
+    print("case: generator", flush=True)
+    x = torch.randn(2, 20, 30, generator=gen(6)).cuda()
+    assert torch.equal(ivf.ivf_orthogonalise(x, (c for c in POLAR[:3])), ivf.ivf_orthogonalise(x, POLAR[:3]))
+    with pytest.raises(ivf.IvfError):
+        ivf.ivf_orthogonalise(x, (c for c in [(1.5, -0.5, 0.0), (1.5, -0.5)]))
+    with pytest.raises(ivf.IvfError):
+        ivf.ivf_orthogonalise(x, (c for c in [(1.5, -0.5, 0.0), (1.5, -0.5, 0.1, 0.2)]))
+    with pytest.raises(ivf.IvfError):
+        ivf.ivf_orthogonalise(x, POLAR, out="x")
