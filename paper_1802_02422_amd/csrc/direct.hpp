@@ -107,7 +107,7 @@ struct DirectLoader {
 template <bool COLS_A, int TERMS_A, int BA, int WA, bool COLS_B, int TERMS_B, int BB, int WB, int BK, int BUFS, bool HALF>
 struct DirectTile {
     static constexpr int NT = WAVE * WA * WB;
-    static constexpr int FA = BA / WA / 32, FB = BB / WB / 32, ROWS_A = BA;
+    static constexpr int FA = BA / WA / 32, FB = BB / WB / 32;
     static constexpr int MOST = TERMS_A > TERMS_B ? TERMS_A : TERMS_B;
     static_assert(BK % 32 == 0, "the fragments change places an even number of times a step");
     using LA = DirectLoader<COLS_A, BA, BK, NT, TERMS_A>;

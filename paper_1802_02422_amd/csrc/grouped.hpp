@@ -110,8 +110,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(APART && BX
     P t;
     t.clear();
     if (p.group < g.G) {
-        Source sw{g.w + ((int64_t)p.group * g.R * g.C + (TRANSPOSED ? (int64_t)c0 : (int64_t)c0 * g.C)) * E::bytes, nullptr, g.C, 0, cols - c0 < BW ? cols - c0 : BW};
-        Source sx{g.x + p.row * g.ldx * E::bytes, nullptr, g.ldx, 0, p.rows};
+        Source sw{g.w + ((int64_t)p.group * g.R * g.C + (TRANSPOSED ? (int64_t)c0 : (int64_t)c0 * g.C)) * E::bytes, nullptr, g.C, cols - c0 < BW ? cols - c0 : BW};
+        Source sx{g.x + p.row * g.ldx * E::bytes, nullptr, g.ldx, p.rows};
         t.product(sw, sx, 0, K, lds);
     }
     const bool bad = T == Type::F32 && any_nan(t);
@@ -348,8 +348,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void g
     const int c0 = j * BC, r0 = i * BR;
     P t;
     t.clear();
-    Source sx{g.x + (p.row * g.ldx + c0) * E::bytes, nullptr, g.ldx, 0, g.C - c0 < BC ? g.C - c0 : BC};
-    Source sd{g.dy + (p.row * g.lddy + r0) * E::bytes, nullptr, g.lddy, 0, g.R - r0 < BR ? g.R - r0 : BR};
+    Source sx{g.x + (p.row * g.ldx + c0) * E::bytes, nullptr, g.ldx, g.C - c0 < BC ? g.C - c0 : BC};
+    Source sd{g.dy + (p.row * g.lddy + r0) * E::bytes, nullptr, g.lddy, g.R - r0 < BR ? g.R - r0 : BR};
     t.product(sx, sd, 0, p.rows, lds);
     const bool bad = T == Type::F32 && any_nan(t);
     store_gradient(t, g, p, r0, c0, lds);

@@ -288,9 +288,9 @@ __global__ __launch_bounds__(256) void mx4_rows_product_kernel(Mx4RowsArgs g, Mx
     const int part = (int)(place / (across * down));
     P t;
     t.clear();
-    Source sb = EXPANDED ? Source{reinterpret_cast<const uint8_t *>(values.p + j0), nullptr, values.ld, 0, (int)(cols - j0 < BN ? cols - j0 : BN)} : Source{TRANSPOSED ? g.codes + j0 / 2 : g.codes + j0 * blocks * 16, TRANSPOSED ? g.scales + j0 / 32 : g.scales + j0 * blocks, (int64_t)blocks * 16, 0,
+    Source sb = EXPANDED ? Source{reinterpret_cast<const uint8_t *>(values.p + j0), nullptr, values.ld, (int)(cols - j0 < BN ? cols - j0 : BN)} : Source{TRANSPOSED ? g.codes + j0 / 2 : g.codes + j0 * blocks * 16, TRANSPOSED ? g.scales + j0 / 32 : g.scales + j0 * blocks, (int64_t)blocks * 16,
               (int)(cols - j0 < BN ? cols - j0 : BN)};
-    Source sa{g.a + i0 * g.lda * E::bytes, nullptr, g.lda, 0, (int)(g.m - i0 < BM ? g.m - i0 : BM)};
+    Source sa{g.a + i0 * g.lda * E::bytes, nullptr, g.lda, (int)(g.m - i0 < BM ? g.m - i0 : BM)};
     const int64_t from = TRANSPOSED ? part * g.part_rows : 0;
     const int64_t to = TRANSPOSED ? (from + g.part_rows < g.n ? from + g.part_rows : g.n) : g.D;
     t.product(sb, sa, from, to, lds);

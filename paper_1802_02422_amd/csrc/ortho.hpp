@@ -351,7 +351,7 @@ __global__ __launch_bounds__(256) void ortho_general_kernel(uint32_t first, Orth
     const int64_t matrix = place / (across * down), size = (int64_t)g.rows_p * g.rows_q;
     const int i0 = (int)(place % across) * 64, j0 = (int)(place / across % down) * 64;
     auto source = [&](const float *p, int rows, int row) {
-        return Source{reinterpret_cast<const uint8_t *>(p + (matrix * rows + row) * g.K), nullptr, g.K, 0, rows - row < 64 ? rows - row : 64};
+        return Source{reinterpret_cast<const uint8_t *>(p + (matrix * rows + row) * g.K), nullptr, g.K, rows - row < 64 ? rows - row : 64};
     };
     P t;
     t.clear();

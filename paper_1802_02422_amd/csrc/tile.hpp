@@ -28,8 +28,7 @@ typedef uint32_t wordx4 __attribute__((ext_vector_type(4)));
 
 // How an operand's element (r, k), k the index that is summed over, lies in memory:
 //   *_ROWS  at r * ld + k;  *_COLS  at k * ld + r;  X4_*: rows of 4-bit values with scale bytes, ld bytes of codes and ld / 16 scales a row
-//   TERMS_ROWS: bfloat16 terms already, term t at t * plane + r * ld + k, ld a multiple of 8 with zeros past K
-enum class Form { H_ROWS, H_COLS, F_ROWS, F_COLS, HALF_ROWS, X4_ROWS, X4_COLS, TERMS_ROWS };
+enum class Form { H_ROWS, H_COLS, F_ROWS, F_COLS, HALF_ROWS, X4_ROWS, X4_COLS };
 
 // Words at any address of global memory (the hardware takes them unaligned).
 template <class W>
@@ -47,7 +46,6 @@ struct Source {
     const uint8_t *p;          // element (0, 0) of the tile's first row
     const uint8_t *scale;      // X4: its scale byte
     int64_t ld;
-    int64_t plane;             // TERMS_ROWS: elements between terms
     int rows;                  // rows that exist, from the first on: others count as zeros
 };
 
@@ -122,9 +120,9 @@ struct Loader {
     static constexpr bool HALVES = FORM == Form::H_ROWS || FORM == Form::HALF_ROWS;
     static constexpr bool COLS = FORM == Form::H_COLS || FORM == Form::F_COLS;   // an item: 8 k of two neighbouring rows
     static constexpr int ITEM_COUNT = COLS ? ROWS / 2 * CH : FORM == Form::X4_ROWS ? ROWS * CH / 4
-                                      : FORM == Form::X4_COLS ? ROWS / 8 * CH : FORM == Form::TERMS_ROWS ? ROWS * CH * TERMS : ROWS * CH;
+                                      : FORM == Form::X4_COLS ? ROWS / 8 * CH : ROWS * CH;
     static constexpr int ITEMS = (ITEM_COUNT + NT - 1) / NT;
-    static constexpr int WORDS = HALVES || FORM == Form::TERMS_ROWS ? 4 : FORM == Form::X4_ROWS ? 5 : FORM == Form::X4_COLS || FORM == Form::F_COLS ? 16 : 8;
+    static constexpr int WORDS = HALVES ? 4 : FORM == Form::X4_ROWS ? 5 : FORM == Form::X4_COLS || FORM == Form::F_COLS ? 16 : 8;
     static constexpr int LDS_HALVES = TERMS * ROWS * BK;
     uint32_t w[ITEMS][WORDS];
 
@@ -196,7 +194,7 @@ struct Loader {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = q[j];
                 v[4] = s.scale[row * (s.ld / 16) + block];
-            } else if constexpr (FORM == Form::X4_COLS) {
+            } else {
                 const int r = 8 * (id % (ROWS / 8));
                 const int64_t k = k0 + (id / (ROWS / 8)) * 8;
                 if (r >= s.rows) continue;
@@ -206,13 +204,6 @@ struct Loader {
                         v[j] = *reinterpret_cast<const uint32_t *>(s.p + (k + j) * s.ld + r / 2);
                         v[8 + j] = s.scale[(k + j) * (s.ld / 16) + r / 32];
                     }
-            } else {
-                const int row = id / CH % ROWS, term = id / (CH * ROWS);
-                const int64_t k = k0 + (id % CH) * 8;
-                if (row >= s.rows || k >= K) continue;
-                const wordx4 q = *reinterpret_cast<const wordx4 *>(reinterpret_cast<const uint16_t *>(s.p) + term * s.plane + row * s.ld + k);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = q[j];
             }
         }
     }
@@ -229,8 +220,6 @@ struct Loader {
             };
             if constexpr (FORM == Form::H_ROWS) {
                 put(0, id / CH, id % CH, wordx4{v[0], v[1], v[2], v[3]});
-            } else if constexpr (FORM == Form::TERMS_ROWS) {
-                put(id / (CH * ROWS), id / CH % ROWS, id % CH, wordx4{v[0], v[1], v[2], v[3]});
             } else if constexpr (FORM == Form::H_COLS) {
                 const int r = 2 * (id % (ROWS / 2)), c = id / (ROWS / 2);
                 put(0, r, c, wordx4{low_halves(v[0], v[1]), low_halves(v[2], v[3]), low_halves(v[4], v[5]), low_halves(v[6], v[7])});
@@ -449,7 +438,6 @@ template <Form FORM_A, int TERMS_A, int BA, int WA, Form FORM_B, int TERMS_B, in
 struct Tile {
     static constexpr int NT = WAVE * WA * WB;
     static constexpr int FA = BA / WA / 32, FB = BB / WB / 32;       // accumulators of a wavefront
-    static constexpr int ROWS_A = BA;
     static constexpr int MOST = TERMS_A > TERMS_B ? TERMS_A : TERMS_B;
     using LA = Loader<FORM_A, BA, BK, NT, TERMS_A, TERMS_B == 1>;
     using LB = Loader<FORM_B, BB, BK, NT, TERMS_B, TERMS_A == 1>;
