@@ -45,3 +45,24 @@ def test_grouped_gradient_as_accurate_as_32_bits(rows):
     err, plain = (got - ref).norm().item(), (torch.bmm(a, b) - ref).norm().item()
     print("error", err, "in fp32", plain, flush=True)
     assert err <= plain
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("R,C", [(400, 700), (513, 385), (129, 1030)])
+def test_grouped_gradient_of_many_tiles(R, C, dtype):
+    """Eight tiles of 128 x 128 and more, dealt to the XCDs by slices: ragged ends, long, short and empty groups, lines that are no whole words."""
+    print("case: tiles", R, C, dtype, flush=True)
+    sizes = [300, 0, 1, 1100, 77]
+    n, g = sum(sizes), gen(R)
+    dy, x = torch.randn(n, R + 1, generator=g, device="cuda").to(dtype)[:, 1:], torch.randn(n, C + 3, generator=g, device="cuda").to(dtype)[:, 2:-1]
+    off = torch.tensor([0] + sizes).cumsum(0).int().cuda()
+    got = ivf.ivf_grouped_gradient(dy, x, off, out_dtype=torch.float32)
+    assert torch.equal(got, ivf.ivf_grouped_gradient(dy, x, off, out_dtype=torch.float32))
+    at = 0
+    for i, s in enumerate(sizes):
+        a, b = dy[at:at + s].double(), x[at:at + s].double()
+        ref, size = a.t().contiguous() @ b, a.abs().t().contiguous() @ b.abs()
+        # a rounding of 2^-23 of the sum so far for 16 products, and of the pieces' sums; fp32 leaves 2^-21 of each product out as well
+        tol = size * ((2.0 ** -20 if dtype == torch.float32 else 0.0) + 2 * (s / 16 + 8) * 2.0 ** -23) + 1e-37
+        assert ((got[i].double() - ref).abs() <= tol).all()
+        at += s
