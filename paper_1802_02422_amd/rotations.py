@@ -16,6 +16,7 @@ from . import binding as B
 POLAR = [(1.875, -1.25, 0.375)] * 12
 
 
+@torch.no_grad()
 def learn(x: torch.Tensor, offsets: torch.Tensor, rounds: int = 8, hold: float = 0.05, start: torch.Tensor | None = None):
     """Rotations [G, D, D] fp32 for the rows x [n, D] fp32, group by group at ``offsets`` [G + 1], and the mean squared error of their 4-bit
     values after every round.  ``hold`` (of a cross-covariance's norm over sqrt(D)) draws towards the rotation of the round before, which
@@ -34,6 +35,7 @@ def learn(x: torch.Tensor, offsets: torch.Tensor, rounds: int = 8, hold: float =
     return R, torch.stack(errors)
 
 
+@torch.no_grad()
 def keep(x: torch.Tensor, R: torch.Tensor, offsets: torch.Tensor) -> B.Mx4Rows:
     """The rows x, rotated by their groups' matrices, in 4 bits."""
     return B.ivf_mx4_quantise(B.ivf_grouped_product(x, R, offsets))

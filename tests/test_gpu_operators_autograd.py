@@ -106,3 +106,15 @@ def test_no_gradient_is_refused():
         with torch.no_grad():
             f()
     assert not ivf.ivf_orthogonalise(x.detach(), [(1.5, -0.5, 0.0)]).requires_grad
+
+
+def test_rotations_are_learned_from_rows_that_ask_for_gradients():
+    """By turns, not by descent: nothing of it is followed."""
+    print("case: rotations", flush=True)
+    from paper_1802_02422_amd import rotations
+    x = torch.randn(60, 32, device="cuda", requires_grad=True)
+    off = torch.tensor([0, 25, 60], dtype=torch.int32, device="cuda")
+    R, errors = rotations.learn(x, off, rounds=2)
+    same, _ = rotations.learn(x.detach(), off, rounds=2)
+    assert torch.equal(R, same) and not R.requires_grad and not errors.requires_grad
+    assert torch.equal(rotations.keep(x, R, off).codes, rotations.keep(x.detach(), R, off).codes)
