@@ -193,6 +193,7 @@ struct DirectTile {
     // acc += a b^T over k in [0, K): a ring of BUFS buffers, BUFS - 1 steps' copies on their way (past K zeros, so that their number is always
     // the same).  One barrier a step, before the products of its last sub-step: everyone has the fragments for those by then, so that the
     // step's buffer is free for the next copies, and everyone's copies of the next step have landed, whose first fragments come while they run.
+    // (Columns: the compiler waits for all copies before a step's first transposing read, as if that depended on them, so they are drained one to three products after they were issued.)
     __device__ __forceinline__ void product(const DirectSource &sa, const DirectSource &sb, int64_t K, uint16_t *lds)
     {
         if (K <= 0) return;

@@ -124,7 +124,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(APART && BX
 }
 
 // The same for 16-bit rows and matrices whose lines are whole 16-byte words: 8192 rows, 32 matrices of 2048 x 2048 in bfloat16 128 us, 540 TFLOP/s with groups of
-// unequal size, bound by reads from LDS (a third more cycles than the products of tiles of 64 x 64 a wavefront take).  The workgroups that an XCD runs at a time share rows of x and of W
+// unequal size.  Transposed (8192 rows, 16 of 2048 x 1024: 62 us) the units are busy for 62 % of the time and the matrix units for 39 % of that: the step's copies are waited for before the
+// first columns are read.  The workgroups that an XCD runs at a time share rows of x and of W
 // (tile_of_place).
 template <bool HALF, bool TRANSPOSED, int BX, int BW, int WX, int WW, int BK, int BUFS>
 __global__ __launch_bounds__(WAVE *WX *WW) void grouped_product_direct_kernel(GroupedArgs g, int pieces)
@@ -149,7 +150,8 @@ __global__ __launch_bounds__(WAVE *WX *WW) void grouped_product_direct_kernel(Gr
 }
 
 // The same for large groups by tiles of 256 x 256, not transposed: 16 384 rows, 8 matrices of 4096 x 2048 in bfloat16 285 us, 963 TFLOP/s (338 by tiles of
-// 128 x 256), 32 matrices 359 us.  Bound by a workgroup's first loads and its stores, during which its compute unit has nothing else.
+// 128 x 256), 32 matrices 365 - 380 us.  Bound by a workgroup's first loads and its stores, during which its compute unit has nothing else, and by a last round of tiles for
+// part of the units: those are busy for 63 % of the time, the matrix units for 61 % of that.
 template <bool HALF>
 __global__ __launch_bounds__(256) void grouped_product_wide_kernel(GroupedArgs g, int pieces)
 {
@@ -329,7 +331,9 @@ __device__ __forceinline__ void store_gradient(const P &t, const GradientArgs &g
         t.store(gradient_part(g, p) + at, g.C, g.R - r0, g.C - c0, Type::F32, lds);
 }
 
-// Both operands by columns.  500 000 rows of 96 fp32 components in 4096 groups: 198 us, bound by the latency of a short group's steps.
+// Both operands by columns.  500 000 rows of 96 fp32 components in 4096 groups: 205 us in long runs (245 from cold clocks), bound by the latency of a short group's steps: the
+// matrix units are busy for 16 % of the units' time.  Sums apart cost a third wavefront a SIMD (170 us with one sum for all products; 200 to 215 with a sum for each 16 rows that is added by
+// itself, 455 by eight wavefronts of half the tile).
 template <Type T, int BR, int BC>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void grouped_gradient_kernel(GradientArgs g)
 {

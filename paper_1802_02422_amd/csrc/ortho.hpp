@@ -8,7 +8,7 @@
 // begin with).  Two terms hold 22 bits of what is within 2^18 of the scale, and the first alone would drift away from matrices that shrink.  Scales are powers of two.
 // Where a step's bounds say little (one that may take singular values past 16, or small
 // ones down faster than by half: ortho_bounded) matrices stay in fp32 and are multiplied as three bfloat16 terms.  One term would leave 2^-12, and after the growth of small singular values up to
-// 2.4e-3 of the result, more than a result in bfloat16 is rounded by; two leave 5e-7 (fp32 products of fp32 values: 3e-6).
+// 2.4e-3 of the result, more than a result in bfloat16 is rounded by; two leave 2e-6 (2048 x 1024 of noise, five steps; the same in fp32 3.3e-6).
 #pragma once
 #include "direct.hpp"
 
@@ -229,7 +229,7 @@ __device__ __forceinline__ DirectSource ortho_source(const OrthoMatrix &m, int64
 template <int B, int W>
 using OrthoTile = DirectTile<false, ORTHO_TERMS, B, W, false, ORTHO_TERMS, B, W, 32, 2, true>;
 
-// 2048 x 4096: A 81 us, A^2 46, the product with Y 101 (780 TFLOP/s of terms' products in the last).
+// 2048 x 4096: A 82 us, A^2 46, the product with Y 102 (630, 560 and 1010 TFLOP/s of terms' products; the matrix units are busy for 36, 31 and 56 % of the units' time).
 // Symmetric results, the tiles on and below the diagonal, each written to both sides.
 //   GRAM: to = Y Y^T, or a I + b Y Y^T (direct)      else: to = a I + b F + c F F, F symmetric
 template <int B, int W, bool GRAM>

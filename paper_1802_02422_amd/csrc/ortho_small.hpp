@@ -9,6 +9,9 @@
 // Scales are powers of two that bring a matrix's largest element, as it is, to 2^13 .. 2^15: of A the largest on its diagonal, of F that of a wavefront's own
 // rows (nobody else has them), of Y that of all of it.  So nothing has to be known of the coefficients: what bounds of the singular values would allow drifts away from what
 // they are when a matrix shrinks for many steps, and two fp16 terms hold 22 bits only of what is within 2^18 of their scale.
+//
+// 4096 x 96 x 96 fp32, ten steps: 805 - 820 us in long runs (900 from cold clocks), the matrix units busy for 37 % of it, LDS for 35; the rest cuts values into terms and waits at
+// barriers.  Three wavefronts a SIMD, for which 25 registers are spilled.  1.2e-7 of the result against 64 bits, the same steps in fp32 1.1e-7.
 #pragma once
 #include "direct.hpp"
 #include "ortho.hpp"

@@ -115,7 +115,8 @@ extern "C" int ivf_grouped_product(const void *x, int64_t ldx, int64_t n, const 
                 // Tiles of 256 x 256 fill the units with half as many and leave more of the last ones empty, and their first loads and stores are hidden by nothing,
                 // so: long sums, large groups, half the units at least.  Against the others: 2048 rows, 4 matrices of 4096 x 2048 56 us to 63, 16 384 rows and 32 of
                 // them 372 to 406, 8192 rows, 8 of 1024 x 4096 85 to 114; but 8192 rows, 16 of 2048 x 1024 62 to 53, 32 of 2048 x 2048 146 to 130, 4096 rows, 4
-                // of 1024 x 2048 48 to 34.
+                // of 1024 x 2048 48 to 34.  In between (256 to 768 rows a group, 1024 to 2048 terms) they are within 10 % of each other but where one of them needs one round of the units more:
+                // 6144 rows, 16 of 1024 x 4096 80 to 109, 12 288 of them 169 to 124.
                 // Transposed products read W by columns, with twice the reads: 470 us by such tiles, 404 by the others, for 16 384 rows and 16 of 4096 x 2048.
                 if (!transposed && C >= 2048 && n / G >= 512 && n / 256 * ceil_div(cols, 256) >= 128)
                     return direct(grouped_product_wide_kernel<HALF>, 256, 256, 256);
