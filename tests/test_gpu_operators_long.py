@@ -14,6 +14,9 @@ F32, BF16 = torch.float32, torch.bfloat16
 
 @pytest.fixture(autouse=True)
 def room():
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("100 GB of free memory are needed")
     yield
     torch.cuda.empty_cache()
 
