@@ -280,8 +280,13 @@ int ortho_general(const void *x, int64_t batch, int rows, int cols, int steps, c
     };
     for (int s = 0; s < steps; ++s) {
         const float *c = coefs + 3 * s;
-        if (int rc = product({y, y, p.m, p.m, p.n, 1.f, 0.f, 0.f, nullptr, a, nullptr, nullptr, T, 0})) return rc;
-        if (int rc = product({a, a, p.m, p.m, p.m, c[2], c[1], c[0], a, f, nullptr, nullptr, T, 0})) return rc;
+        // (without a last coefficient A^2, which may leave fp32's range, is not formed)
+        if (c[2] == 0.f) {
+            if (int rc = product({y, y, p.m, p.m, p.n, c[1], 0.f, c[0], nullptr, f, nullptr, nullptr, T, 0})) return rc;
+        } else {
+            if (int rc = product({y, y, p.m, p.m, p.n, 1.f, 0.f, 0.f, nullptr, a, nullptr, nullptr, T, 0})) return rc;
+            if (int rc = product({a, a, p.m, p.m, p.m, c[2], c[1], c[0], a, f, nullptr, nullptr, T, 0})) return rc;
+        }
         if (int rc = product({yt, f, p.n, p.m, p.m, 1.f, 0.f, 0.f, nullptr, y, yt2, s + 1 == steps ? out : nullptr, T, turned})) return rc;
         std::swap(yt, yt2);
     }

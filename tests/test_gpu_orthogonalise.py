@@ -175,3 +175,10 @@ def test_coefficients_from_a_generator():
         ivf.ivf_orthogonalise(x, (c for c in [(1.5, -0.5, 0.0), (1.5, -0.5, 0.1, 0.2)]))
     with pytest.raises(ivf.IvfError):
         ivf.ivf_orthogonalise(x, POLAR, out="x")
+
+
+@pytest.mark.parametrize("shape", [(2, 60, 40), (1, 150, 140), (2, 90, 300)])
+def test_no_square_without_its_coefficient(shape):
+    """A^2 would leave the range of 32 bits where the result, which has none of it, does not."""
+    print("case: no square", shape, flush=True)
+    check(torch.randn(*shape, generator=gen(8)), [(1e11, 0.0, 0.0), (1.0, 1e-10, 0.0)], eps=0.0)
